@@ -67,8 +67,10 @@ typedef enum {
 typedef enum {
     DT_OUT_CLASS_U8 = 0,      /* uint8_t label per record; requires n_classes <= 256      */
     DT_OUT_CLASS_I32 = 1,     /* int32_t label per record                                   */
-    DT_OUT_LEAF_I32 = 2       /* int32_t index (in the node array) of the leaf reached;
+    DT_OUT_LEAF_I32 = 2,      /* int32_t index (in the node array) of the leaf reached;
                                  single trees only                                          */
+    DT_OUT_VOTES_U8 = 3       /* n_classes uint8_t per record: each class's number of trees;
+                                 dt_forest_classify only                                    */
 } dt_output;
 
 /*
@@ -309,7 +311,9 @@ void dt_forest_destroy(dt_forest *forest);
  * Majority vote of the forest's trees for n records; ties go to the smallest class id
  * (Section 1's forests; each tree evaluated as dt_classify, Sections 3.2-3.4).
  * Arguments, errors, graph capture and concurrent use as dt_classify; out_kind must be
- * DT_OUT_CLASS_U8 or DT_OUT_CLASS_I32.
+ * DT_OUT_CLASS_U8, DT_OUT_CLASS_I32 or DT_OUT_VOTES_U8.  With DT_OUT_VOTES_U8 the trees' votes
+ * are not reduced to a class: d_out has n rows of n_classes uint8 counts without gaps, the form
+ * that the operators of dtree_scores.h take as scores of type DT_U8.
  */
 dt_status dt_forest_classify(const dt_forest *forest, const float *d_x, int64_t n, int64_t ld,
                              void *d_out, dt_output out_kind, dt_algo algo, void *stream);
@@ -395,7 +399,8 @@ dt_status dt_classify_host_typed(const dt_tree *tree, dt_pipeline *pipeline, con
                                  dt_output out_kind, dt_algo algo, dt_pipeline_stats *stats);
 
 /* Outer-time classification (Section 4.2) of a forest's majority vote (Section 1): as
- * dt_classify_host for dt_forest_classify. */
+ * dt_classify_host for dt_forest_classify (classes only: DT_ERR_INVALID_ARG for
+ * DT_OUT_VOTES_U8). */
 dt_status dt_forest_classify_host(const dt_forest *forest, dt_pipeline *pipeline,
                                   const float *h_x, int64_t n, int64_t ld, void *h_out,
                                   dt_output out_kind, dt_algo algo, dt_pipeline_stats *stats);

@@ -816,5 +816,23 @@ __device__ __forceinline__ void store_value(void *out, int out_kind, int64_t n, 
     }
 }
 
+// Vote counts of a record: byte c of the packed counters is class c's, and the record's output
+// row is n_classes bytes.  Whole words where every row starts at a word.
+template <int NV>
+__device__ __forceinline__ void store_votes(void *out, int64_t n, int64_t row, int n_classes,
+                                            const uint32_t (&votes)[NV]) {
+    if (row >= n) return;
+    uint8_t *o = static_cast<uint8_t *>(out) + row * n_classes;
+    if (((uint32_t(n_classes) | uint32_t(reinterpret_cast<uintptr_t>(out))) & 3u) == 0) {
+#pragma unroll
+        for (int r = 0; r < NV; ++r)
+            if (4 * r < n_classes) reinterpret_cast<uint32_t *>(o)[r] = votes[r];
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4 * NV; ++c)
+            if (c < n_classes) o[c] = uint8_t(votes[c >> 2] >> (8 * (c & 3)));
+    }
+}
+
 }  // namespace dev
 }  // namespace dtree

@@ -1103,8 +1103,8 @@ dt_status forest_classify_impl(const dt_forest *f, const float *d_x, int64_t n, 
         return fail(DT_ERR_UNSUPPORTED, "forests run the data and speculative decompositions");
     if (algo != DT_ALGO_DATA && algo != DT_ALGO_SPECULATIVE)
         return fail(DT_ERR_INVALID_ARG, "unknown algo");
-    if (out_kind != DT_OUT_CLASS_U8 && out_kind != DT_OUT_CLASS_I32)
-        return fail(DT_ERR_INVALID_ARG, "forests output classes (uint8 or int32)");
+    if (out_kind != DT_OUT_CLASS_U8 && out_kind != DT_OUT_CLASS_I32 && out_kind != DT_OUT_VOTES_U8)
+        return fail(DT_ERR_INVALID_ARG, "forests output classes (uint8 or int32) or votes");
     if (ld < f->n_features) return fail(DT_ERR_INVALID_ARG, "ld must be >= n_features");
     if (f->n_features > dtree::kMaxRowStride)
         return fail(DT_ERR_UNSUPPORTED, "n_features > 256");
@@ -1142,7 +1142,9 @@ dt_status forest_classify_impl(const dt_forest *f, const float *d_x, int64_t n, 
         a.depth = enc.depth;
         a.n_classes = f->n_classes;
         a.waves = plan.waves;
-        a.out_kind = out_kind == DT_OUT_CLASS_U8 ? 0 : 1;
+        a.out_kind = out_kind == DT_OUT_CLASS_U8   ? 0
+                     : out_kind == DT_OUT_VOTES_U8 ? dtree::kOutVotes
+                                                   : 1;
         a.out = d_out;
         const int64_t groups = (end - first + plan.tiles - 1) / plan.tiles;
         const int64_t resident = int64_t(plan.blocks_per_cu) * f->caps.n_cu;

@@ -80,6 +80,15 @@ __device__ __forceinline__ int majority(const uint32_t (&votes)[NV], int n_class
     return best;
 }
 
+// A record's answer: the class with the most votes, or all classes' votes.
+template <int NV>
+__device__ __forceinline__ void answer(const FArgs &f, int64_t row, const uint32_t (&votes)[NV]) {
+    if (f.out_kind == kOutVotes)
+        dev::store_votes(f.out, f.in.n, row, f.n_classes, votes);
+    else
+        dev::store_value(f.out, f.out_kind, f.in.n, row, majority(votes, f.n_classes));
+}
+
 // The kernel arguments, for the code around the walk.  The walk needs every scalar register,
 // and the arguments of row tiles held across it spilled to vector lanes (a 32-tree forest
 // 457 us against 373 us): for them the arguments are read again, through a pointer the
@@ -289,8 +298,7 @@ __global__ void __launch_bounds__(64 * forest_max_waves(SD == 0 ? 0 : 1, SD)) fo
         }
         if (active) {
             const FArgs &f = cold_args<Tile>(a);
-            dev::store_value(f.out, f.out_kind, f.in.n, t * kTileRows + lane,
-                             majority(votes, f.n_classes));
+            answer(f, t * kTileRows + lane, votes);
         }
     }
 }
@@ -353,8 +361,7 @@ forest_split_kernel(FArgs a) {
 #pragma unroll
             for (int r = 0; r < NV; ++r) votes[r] = box[64 * r];
             const FArgs &f = cold_args<Tile>(a);
-            dev::store_value(f.out, f.out_kind, f.in.n, t * kTileRows + lane,
-                             majority(votes, f.n_classes));
+            answer(f, t * kTileRows + lane, votes);
         }
     }
 }

@@ -121,9 +121,10 @@ struct FArgs {
     int32_t depth;           // window depth D (every tree)
     int32_t n_classes;
     int32_t waves;
-    int32_t out_kind;        // 0: uint8 output, 1: int32 output
+    int32_t out_kind;        // 0: uint8 output, 1: int32 output, 2: the votes (kOutVotes)
     void *out;
 };
+constexpr int kOutVotes = 2;
 
 // How record tiles are read from HBM.  Single-tree kernels:
 //   kLoadExact  dense rows of a power of two of words (4 to 64), 16-byte aligned base

@@ -504,6 +504,8 @@ dt_status dt_forest_classify_host(const dt_forest *forest, dt_pipeline *pipeline
                                   dt_output out_kind, dt_algo algo, dt_pipeline_stats *stats) {
     try {
         dtree::clear_error();
+        if (out_kind == DT_OUT_VOTES_U8)
+            return set_error(DT_ERR_INVALID_ARG, "host-resident records are answered with classes");
         const int32_t F = pipeline ? pipeline->n_features : 0;
         const ClassifyFn fn = [=](const void *d_x, int64_t rows, void *d_out, hipStream_t s) {
             return dt_forest_classify(forest, static_cast<const float *>(d_x), rows, F, d_out,

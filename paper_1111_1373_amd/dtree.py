@@ -30,7 +30,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 DT_OK, DT_ERR_INVALID_ARG, DT_ERR_INVALID_TREE, DT_ERR_UNSUPPORTED, DT_ERR_HIP, DT_ERR_NO_MEMORY = range(6)
 ALGOS = {"data": 0, "speculative": 1, "path": 2}
-OUT_KINDS = {"class_u8": 0, "class_i32": 1, "leaf_i32": 2}
+OUT_KINDS = {"class_u8": 0, "class_i32": 1, "leaf_i32": 2, "votes_u8": 3}
 X_TYPES = {"f32": 0, "f16": 1, "bf16": 2, "u8": 3}
 
 NODE_DTYPE = np.dtype(
@@ -298,8 +298,18 @@ class Forest:
                "dt_forest_create")
 
     def classify(self, x, algo: str = "data", out_kind: str = "class_u8", out=None, stream=None):
+        """Majority votes of the rows of ``x`` (float32); with ``out_kind="votes_u8"`` every
+        class's number of votes, uint8 [n, n_classes]."""
         ptr, n, ld = _features_arg(x, self.n_features)
-        out = _out_tensor(out, n, out_kind, x.device)
+        if out_kind == "votes_u8":
+            if out is None:
+                out = torch.empty(n, self.n_classes, dtype=torch.uint8, device=x.device)
+            elif out.dtype != torch.uint8 or out.shape != (n, self.n_classes) or \
+                    not out.is_contiguous() or out.device != x.device:
+                raise ValueError("out must be a contiguous uint8 tensor of %d x %d on %s"
+                                 % (n, self.n_classes, x.device))
+        else:
+            out = _out_tensor(out, n, out_kind, x.device)
         _check(_lib.dt_forest_classify(self._h, ptr, n, ld, out.data_ptr() if n else None,
                                        OUT_KINDS[out_kind], ALGOS[algo], _stream_handle(stream)),
                "dt_forest_classify")
