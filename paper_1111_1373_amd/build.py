@@ -1,4 +1,4 @@
-"""Build the gfx950 library ``libdtree.so`` in-tree with hipcc.
+"""Build the gfx950 libraries ``libdtree.so`` and ``libdscores.so`` in-tree with hipcc.
 
     python -m paper_1111_1373_amd.build
 
@@ -21,6 +21,9 @@ OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["dtree.hip", "kernels.hip", "kernels_f16.hip", "kernels_bf16.hip", "kernels_u8.hip",
            "forest.hip", "forest_ex16.hip",
            "forest_packed.hip", "forest_list.hip", "forest_spec.hip", "probe.hip", "path.hip", "encode.cpp", "pipeline.cpp"]
+# operators on rows of class scores: a library of their own, which needs no tree
+SCORES_LIB = os.path.join(HERE, "libdscores.so")
+SCORES_SOURCES = ["scores.cpp", "scores_top.hip", "scores_sample.hip", "scores_distill.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -47,21 +50,26 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every translation unit (in parallel) and link libdtree.so."""
-    from concurrent.futures import ThreadPoolExecutor
-
-    os.makedirs(OBJDIR, exist_ok=True)
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    jobs = max(1, min(len(srcs), os.cpu_count() or 1))
-    with ThreadPoolExecutor(jobs) as pool:
-        objs = list(pool.map(lambda s: _compile(s, verbose), srcs))
-    tmp = LIB + ".tmp%d" % os.getpid()
+def _link(lib: str, objs, verbose: bool) -> None:
+    tmp = lib + ".tmp%d" % os.getpid()
     cmd = [hipcc(), "-shared", "-fPIC", "--hip-link", "--offload-arch=" + ARCH, "-o", tmp] + objs
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    os.replace(tmp, LIB)
+    os.replace(tmp, lib)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every translation unit (in parallel) and link the libraries; returns libdtree.so."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    os.makedirs(OBJDIR, exist_ok=True)
+    srcs = [os.path.join(CSRC, s) for s in SOURCES + SCORES_SOURCES]
+    jobs = max(1, min(len(srcs), os.cpu_count() or 1))
+    with ThreadPoolExecutor(jobs) as pool:
+        objs = list(pool.map(lambda s: _compile(s, verbose), srcs))
+    _link(LIB, objs[:len(SOURCES)], verbose)
+    _link(SCORES_LIB, objs[len(SOURCES):], verbose)
     return LIB
 
 

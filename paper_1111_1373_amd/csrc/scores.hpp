@@ -1,0 +1,58 @@
+// Internal interface between the translation units of libdscores (not part of the C ABI).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "dtree_scores.h"
+
+namespace dscores {
+
+// Rows of few classes are worked on by one lane each, others by teams of 1, 4 or 16 wavefronts.
+constexpr int kLaneClasses = 64;
+
+struct RowArgs {
+    const void *x;
+    int64_t n, ld;
+    int32_t classes;
+    int32_t align;        // every row starts at a multiple of this many bytes (1 .. 16)
+};
+
+struct TopArgs {
+    RowArgs in;
+    int32_t k;
+    float *values;
+    int32_t *index;
+    float *lse;
+};
+
+struct SampleArgs {
+    RowArgs in;
+    const float *u;
+    ds_sampling set;
+    int32_t *labels;
+};
+
+struct DistillArgs {
+    RowArgs in;
+    const float *values;
+    const int32_t *index;
+    int32_t k;
+    float temperature;
+    const float *g;
+    float *loss;
+    float2 *stats;        // (largest score, sum of e^((x - largest) / temperature)) of each row
+    void *grad;
+    int64_t ld_grad;
+    float2 *part;         // the same of each part of each row
+    int32_t parts;        // of a row
+};
+
+hipError_t launch_top(const TopArgs &a, dt_dtype type, hipStream_t stream);
+hipError_t launch_sample(const SampleArgs &a, dt_dtype type, hipStream_t stream);
+hipError_t launch_distill(const DistillArgs &a, dt_dtype type, hipStream_t stream);
+hipError_t launch_distill_backward(const DistillArgs &a, dt_dtype type, hipStream_t stream);
+int distill_parts(int64_t n, int32_t classes);
+
+}  // namespace dscores

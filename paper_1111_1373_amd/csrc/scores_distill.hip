@@ -1,0 +1,351 @@
+// Distillation from a teacher's top scores (ds_distill, ds_distill_backward).
+//
+// With m the row's largest score and s = sum e^((x - m) / t), q_c = e^((x_c - m) / t) / s.  One
+// pass over a row finds m and s together: each thread keeps the largest score it has met and the
+// sum relative to it, scaled down when a larger one comes.  The gradient takes a second pass:
+// every class gets g t q_c, then the teacher's classes (at most 256 a row) are written again
+// with their share of p taken off.  An entry whose class another entry has too adds up all of
+// them in the entries' order, so both write the same number.
+#include "scores.hpp"
+#include "scores_common.hpp"
+
+namespace dscores {
+namespace {
+
+constexpr int kLossOnly = 0, kBoth = 1, kGradOnly = 2;
+
+// G lanes of a wavefront, or a workgroup of G threads, that work on one row.
+template <int G>
+struct Group {
+    static constexpr int kInBlock = G <= 64 ? 256 / G : 1;
+    static constexpr int kThreads = G <= 64 ? 256 : G;        // of the workgroup
+    int thread;
+    float *box;                     // G / 64 words, where G > 64
+
+    __device__ __forceinline__ void sync() const {
+        if constexpr (G <= 64) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        } else {
+            __syncthreads();
+        }
+    }
+    template <class Op>
+    __device__ __forceinline__ float reduce(float v, Op op) const {
+        v = wave_reduce(v, op, G < 64 ? G : 64);
+        if constexpr (G > 64) {
+            sync();
+            if ((thread & 63) == 0) box[thread >> 6] = v;
+            sync();
+            v = box[0];
+#pragma unroll
+            for (int w = 1; w < G / 64; ++w) v = op(v, box[w]);
+        }
+        return v;
+    }
+};
+
+// fmaxf leaves out a NaN, which a sum of exponentials keeps.
+struct MaxNum {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// The largest of some scores, and the sum of e^((x - largest) / t) over them.
+struct Stats {
+    float m = -__builtin_inff(), s = 0.0f;
+
+    // x - m where m may be -inf (then x is too, or NaN)
+    static __device__ __forceinline__ float below(float x, float m) {
+        return x - (m == -__builtin_inff() ? 0.0f : m);
+    }
+    __device__ __forceinline__ void raise(float m1, float inv) {
+        if (m1 > m) {
+            s *= exp_neg(below(m, m1) * inv);
+            m = m1;
+        }
+    }
+    __device__ __forceinline__ void add(float x, float inv) {
+        raise(x, inv);
+        s += exp_neg(below(x, m) * inv);
+    }
+    template <dt_dtype XT>
+    __device__ __forceinline__ void add(const Row<XT> &row, const u32x4 &a, float inv) {
+        using E = Elem<XT>;
+        float x[Row<XT>::kVec], top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < Row<XT>::kVec; ++i) {
+            x[i] = E::wide(row.at(a, i));
+            top = fmaxf(top, x[i]);
+        }
+        raise(top, inv);
+        const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < Row<XT>::kVec; ++i) s += exp_neg((x[i] - base) * inv);
+    }
+    template <class Gr>
+    __device__ __forceinline__ void join(const Gr &g, float inv) {
+        raise(g.reduce(m, MaxNum()), inv);
+        s = g.reduce(s, Sum());
+    }
+    // without any score above -inf (a NaN counts as one)
+    __device__ __forceinline__ bool empty() const { return m == -__builtin_inff() && s == 0.0f; }
+};
+
+// The teacher's entries of one row: their classes (-1: left out) and weights, in the LDS.
+struct Entries {
+    int *cls;
+    float *p;
+};
+
+// Fills them in; returns whether there are any, and the row's loss (the first thread's).
+template <dt_dtype XT, int MODE, class Gr>
+__device__ __forceinline__ bool teach(const DistillArgs &a, const Gr &g, int threads, int64_t r,
+                                      const Row<XT> &row, const Stats &st, const Entries &e,
+                                      float *loss) {
+    const float inv = 1.0f / a.temperature;
+    const float *values = a.values + r * a.k;
+    const int32_t *index = a.index + r * a.k;
+    float top = -__builtin_inff(), any = 0.0f;
+    for (int j = g.thread; j < a.k; j += threads) {
+        const float v = values[j];
+        const int c = index[j];
+        const bool in = c >= 0 && c < a.in.classes && v != -__builtin_inff();
+        e.cls[j] = in ? c : -1;
+        e.p[j] = v;
+        if (in) {
+            any = 1.0f;
+            top = fmaxf(top, v);
+        }
+    }
+    any = g.reduce(any, MaxNum());
+    top = g.reduce(top, MaxNum());
+    float sum = 0.0f;
+    for (int j = g.thread; j < a.k; j += threads)
+        if (e.cls[j] >= 0) sum += exp_neg((e.p[j] - top) * inv);
+    sum = g.reduce(sum, Sum());
+    const float log_sum = logf(sum), log_s = MODE == kGradOnly ? 0.0f : logf(st.s);
+    float l = 0.0f;
+    for (int j = g.thread; j < a.k; j += threads) {
+        float p = 0.0f;
+        const int c = e.cls[j];
+        if (c >= 0) {
+            const float d = (e.p[j] - top) * inv;
+            p = exp_neg(d) / sum;
+            if constexpr (MODE != kGradOnly) {
+                const float logq = Stats::below(Elem<XT>::wide(row.p[c]), st.m) * inv - log_s;
+                if (p != 0.0f) l += p * (d - log_sum - logq);
+            }
+        }
+        e.p[j] = p;
+    }
+    if constexpr (MODE != kGradOnly) {
+        l = g.reduce(l, Sum());
+        *loss = any != 0.0f && !st.empty() ? a.temperature * a.temperature * l : 0.0f;
+    }
+    g.sync();                          // the entries are written
+    return any != 0.0f;
+}
+
+// Gradient of the classes of the vectors [lo, hi) of a row.
+template <dt_dtype XT, class Gr>
+__device__ __forceinline__ void gradient(const DistillArgs &a, const Gr &g, int threads, int64_t r,
+                                         const Row<XT> &row, int lo, int hi, const Stats &st,
+                                         bool taught, const Entries &e) {
+    using E = Elem<XT>;
+    using Raw = typename E::Raw;
+    const float inv = 1.0f / a.temperature;
+    Raw *out = static_cast<Raw *>(a.grad) + r * a.ld_grad;
+    const bool some = taught && !st.empty();
+    const float base = st.m == -__builtin_inff() ? 0.0f : st.m;
+    const float gt = a.g[r] * a.temperature;
+    const float scale = gt / st.s;
+    auto of = [&](float x) { return some ? exp_neg((x - base) * inv) * scale : 0.0f; };
+    // 16-byte stores where the gradient's row lies between 16-byte boundaries as the scores' does
+    const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
+    row.template walk<2>(
+        lo, hi, g.thread, threads,
+        [&](const u32x4 &v4, int v) {
+            constexpr int kPerWord = 4 / E::kBytes;
+            u32x4 q = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < Row<XT>::kVec; ++i)
+                q[i / kPerWord] |= uint32_t(E::narrow(of(E::wide(row.at(v4, i)))))
+                                   << (8 * E::kBytes * (i % kPerWord));
+            Raw *to = out + row.first(v);
+            if (same) {
+                *reinterpret_cast<u32x4 *>(to) = q;
+            } else {
+#pragma unroll
+                for (int i = 0; i < Row<XT>::kVec; ++i) to[i] = row.at(q, i);
+            }
+        },
+        [&](Raw x, int c) { out[c] = E::narrow(of(E::wide(x))); });
+    g.sync();                          // a class's first store comes before its second
+    if (some)
+        for (int j = g.thread; j < a.k; j += threads) {
+            const int c = e.cls[j];
+            if (c < row.first(lo) || c >= row.first(hi) || c < 0) continue;
+            float p = 0.0f;
+            for (int i = 0; i < a.k; ++i)
+                if (e.cls[i] == c) p += e.p[i];
+            const float q = exp_neg((E::wide(row.p[c]) - base) * inv) / st.s;
+            out[c] = E::narrow(gt * (q - p));
+        }
+}
+
+template <dt_dtype XT, int G, int MODE>
+__global__ void __launch_bounds__(Group<G>::kThreads) distill_rows(DistillArgs a) {
+    using Gr = Group<G>;
+    constexpr int kEntries = G == 8 ? kLaneClasses : DS_MAX_TOP;
+    __shared__ int cls[Gr::kInBlock][kEntries];
+    __shared__ float p[Gr::kInBlock][kEntries];
+    __shared__ float box[G > 64 ? G / 64 : 1];
+    const int which = G <= 64 ? int(threadIdx.x) / G : 0;
+    const Gr g{G <= 64 ? int(threadIdx.x) % G : int(threadIdx.x), box};
+    const Entries e{cls[which], p[which]};
+    const float inv = 1.0f / a.temperature;
+    for (int64_t r = int64_t(blockIdx.x) * Gr::kInBlock + which; r < a.in.n;
+         r += int64_t(gridDim.x) * Gr::kInBlock) {
+        const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
+        Stats st;
+        if constexpr (MODE == kGradOnly) {
+            const float2 v = a.stats[r];
+            st.m = v.x;
+            st.s = v.y;
+        } else {
+            row.template walk<4>(
+                0, row.vecs, g.thread, G, [&](const u32x4 &v, int) { st.add(row, v, inv); },
+                [&](auto x, int) { st.add(Elem<XT>::wide(x), inv); });
+            st.join(g, inv);
+            if (g.thread == 0) a.stats[r] = float2{st.m, st.s};
+        }
+        float loss = 0.0f;
+        const bool taught = teach<XT, MODE>(a, g, G, r, row, st, e, &loss);
+        if (MODE != kGradOnly && g.thread == 0) a.loss[r] = loss;
+        if constexpr (MODE != kLossOnly) {
+            const int per = MODE == kGradOnly ? (row.vecs + a.parts - 1) / a.parts : row.vecs;
+            const int lo = MODE == kGradOnly ? int(blockIdx.y) * per : 0;
+            const int hi = lo + per < row.vecs ? lo + per : row.vecs;
+            if (lo < hi) gradient<XT>(a, g, G, r, row, lo, hi, st, taught, e);
+        }
+        g.sync();
+    }
+}
+
+// Long rows, few of them: a workgroup for each part of a row, and a wavefront to join them.
+template <dt_dtype XT>
+__global__ void __launch_bounds__(256) distill_part(DistillArgs a) {
+    __shared__ float box[4];
+    const Group<256> g{int(threadIdx.x), box};
+    const float inv = 1.0f / a.temperature;
+    const Row<XT> row(a.in.x, blockIdx.x, a.in.ld, a.in.classes);
+    const int per = (row.vecs + a.parts - 1) / a.parts;
+    const int lo = int(blockIdx.y) * per < row.vecs ? int(blockIdx.y) * per : row.vecs;
+    const int hi = lo + per < row.vecs ? lo + per : row.vecs;
+    Stats st;
+    if (lo < hi)
+        row.template walk<4>(
+            lo, hi, g.thread, 256, [&](const u32x4 &v, int) { st.add(row, v, inv); },
+            [&](auto x, int) { st.add(Elem<XT>::wide(x), inv); });
+    st.join(g, inv);
+    if (g.thread == 0) a.part[int64_t(blockIdx.x) * a.parts + blockIdx.y] = float2{st.m, st.s};
+}
+
+template <dt_dtype XT>
+__global__ void __launch_bounds__(64) distill_join(DistillArgs a) {
+    __shared__ int cls[DS_MAX_TOP];
+    __shared__ float p[DS_MAX_TOP];
+    const Group<64> g{int(threadIdx.x), nullptr};
+    const float inv = 1.0f / a.temperature;
+    const int64_t r = blockIdx.x;
+    const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
+    Stats st;
+    for (int i = g.thread; i < a.parts; i += 64) {
+        const float2 v = a.part[r * a.parts + i];
+        st.raise(v.x, inv);
+        st.s += v.y * exp_neg(Stats::below(v.x, st.m) * inv);
+    }
+    st.join(g, inv);
+    if (g.thread == 0) a.stats[r] = float2{st.m, st.s};
+    float loss = 0.0f;
+    teach<XT, kLossOnly>(a, g, 64, r, row, st, Entries{cls, p}, &loss);
+    if (g.thread == 0) a.loss[r] = loss;
+}
+
+template <dt_dtype XT, int G, int MODE>
+void run_rows(const DistillArgs &a, hipStream_t stream) {
+    const int64_t blocks = (a.in.n + Group<G>::kInBlock - 1) / Group<G>::kInBlock;
+    distill_rows<XT, G, MODE><<<dim3(unsigned(blocks < 1048576 ? blocks : 1048576), unsigned(a.parts)),
+                                Group<G>::kThreads, 0, stream>>>(a);
+}
+
+// Rows for 8 lanes: few classes, and no more of the teacher's entries than they have room for.
+bool small(const DistillArgs &a) { return a.in.classes <= kLaneClasses && a.k <= kLaneClasses; }
+
+template <dt_dtype XT>
+void run_backward(DistillArgs a, hipStream_t stream) {
+    const int c = a.in.classes;
+    a.parts = 1;
+    if (small(a)) {
+        run_rows<XT, 8, kGradOnly>(a, stream);
+    } else if (c <= 2048) {
+        run_rows<XT, 64, kGradOnly>(a, stream);
+    } else {
+        a.parts = distill_parts(a.in.n, c);
+        run_rows<XT, 256, kGradOnly>(a, stream);
+    }
+}
+
+template <dt_dtype XT>
+void run(const DistillArgs &a, hipStream_t stream) {
+    const int c = a.in.classes;
+    if (a.parts > 1) {
+        const dim3 grid(unsigned(a.in.n), unsigned(a.parts));
+        distill_part<XT><<<grid, 256, 0, stream>>>(a);
+        distill_join<XT><<<unsigned(a.in.n), 64, 0, stream>>>(a);
+        if (a.g) run_backward<XT>(a, stream);
+    } else if (small(a)) {
+        if (a.g) run_rows<XT, 8, kBoth>(a, stream);
+        else run_rows<XT, 8, kLossOnly>(a, stream);
+    } else if (c <= 2048) {
+        if (a.g) run_rows<XT, 64, kBoth>(a, stream);
+        else run_rows<XT, 64, kLossOnly>(a, stream);
+    } else if (c <= 16384) {
+        if (a.g) run_rows<XT, 256, kBoth>(a, stream);
+        else run_rows<XT, 256, kLossOnly>(a, stream);
+    } else {
+        if (a.g) run_rows<XT, 1024, kBoth>(a, stream);
+        else run_rows<XT, 1024, kLossOnly>(a, stream);
+    }
+}
+
+}  // namespace
+
+// Parts of a row: as many as fill the card with workgroups, of 4,096 classes at least.
+int distill_parts(int64_t n, int32_t classes) {
+    if (n >= 512 || classes <= 8192) return 1;
+    const int64_t want = (1024 + n - 1) / n, most = classes / 4096;
+    const int64_t parts = want < most ? want : most;
+    return int(parts < 64 ? parts : 64);
+}
+
+hipError_t launch_distill(const DistillArgs &a, dt_dtype type, hipStream_t stream) {
+    switch (type) {
+        case DT_F32: run<DT_F32>(a, stream); break;
+        case DT_F16: run<DT_F16>(a, stream); break;
+        default: run<DT_BF16>(a, stream); break;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_distill_backward(const DistillArgs &a, dt_dtype type, hipStream_t stream) {
+    switch (type) {
+        case DT_F32: run_backward<DT_F32>(a, stream); break;
+        case DT_F16: run_backward<DT_F16>(a, stream); break;
+        default: run_backward<DT_BF16>(a, stream); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dscores

@@ -1,0 +1,525 @@
+// A class drawn from each row by temperature, top-k, top-p and min-p (ds_sample).
+//
+// Which class a given random number draws is decided by sums of weights, and so are the
+// borders of top-p; with many classes the sums' rounding would decide it.  Weights are
+// therefore computed in 64 bits and rounded once to whole multiples of 2^-42 of the largest
+// one, and added as 64-bit integers (at most 2^20 of them): every order of summation gives the
+// same sum, so the lanes, wavefronts and atomics that share a row cannot change a result.
+#include "scores.hpp"
+#include "scores_lanes.hpp"
+#include "scores_select.hpp"
+
+namespace dscores {
+namespace {
+
+constexpr double kOne = 4398046511104.0;       // 2^42, the weight of a row's best class
+constexpr float kNats = 30.0f;                 // e^-30 rounds to weight 0
+
+// A row's settings, as numbers that mean something.
+struct Settings {
+    double inv;          // 1 / temperature; 0 for temperature 0
+    int k;               // 1 .. n_classes
+    double p;
+    double min_p;
+    bool counts;         // votes at temperature 1
+};
+
+template <dt_dtype XT>
+__device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t row) {
+    const float t = a.set.d_temperature ? a.set.d_temperature[row] : a.set.temperature;
+    const int k = a.set.d_top_k ? a.set.d_top_k[row] : a.set.top_k;
+    const float p = a.set.d_top_p ? a.set.d_top_p[row] : a.set.top_p;
+    const float m = a.set.d_min_p ? a.set.d_min_p[row] : a.set.min_p;
+    Settings s;
+    s.inv = t > 0.0f ? 1.0 / double(t) : 0.0;
+    s.k = !(t > 0.0f) ? 1 : (k < 1 || k > a.in.classes) ? a.in.classes : k;
+    s.p = p < 1.0f ? double(p) : 1.0;                   // NaN: 1
+    s.min_p = m > 0.0f ? double(m < 1.0f ? m : 1.0f) : 0.0;
+    s.counts = XT == DT_U8 && t == 1.0f;
+    return s;
+}
+
+// e^d for -30 <= d <= 0 as a whole multiple of 2^-42.  e^d = 2^n e^r with n the integer next to
+// d / ln 2 and |r| <= ln 2 / 2; e^r by its Taylor sum up to r^11, whose remainder is below
+// 0.3466^12 / 12! = 6.3e-15, 2^-47.  Adding 2^52 leaves the rounded integer in the low bits.
+__device__ __forceinline__ uint64_t exp_weight(double d) {
+    const double n = __builtin_rint(d * 1.4426950408889634);
+    const double r = fma(-n, 0.6931471805599453, d);
+    double e = 1.0 / 39916800.0;
+    e = fma(e, r, 1.0 / 3628800.0);
+    e = fma(e, r, 1.0 / 362880.0);
+    e = fma(e, r, 1.0 / 40320.0);
+    e = fma(e, r, 1.0 / 5040.0);
+    e = fma(e, r, 1.0 / 720.0);
+    e = fma(e, r, 1.0 / 120.0);
+    e = fma(e, r, 1.0 / 24.0);
+    e = fma(e, r, 1.0 / 6.0);
+    e = fma(e, r, 0.5);
+    e = fma(e, r, 1.0);
+    e = fma(e, r, 1.0);
+    const double w = __builtin_amdgcn_ldexp(e, int(n) + 42) + 4503599627370496.0;
+    return __builtin_bit_cast(uint64_t, w) & 0xFFFFFFFFFFFFFull;
+}
+
+// Weights of a row's classes by their keys.
+template <dt_dtype XT>
+struct Weights {
+    uint32_t top;        // the best key
+    double m;            // its score
+    double inv;
+    bool counts;
+    const double *ln;    // ln of 0 .. 255 (votes)
+
+    __device__ __forceinline__ Weights(const Settings &s, uint32_t top_key, const double *ln_table)
+        : top(top_key), inv(s.inv), counts(s.counts), ln(ln_table) {
+        if constexpr (XT == DT_U8)
+            m = ln[top];
+        else
+            m = double(Elem<XT>::value(top));
+    }
+    __device__ __forceinline__ double one() const {
+        return counts ? double(top) * 17179869184.0 : kOne;          // 2^34 a vote
+    }
+    __device__ __forceinline__ uint64_t operator()(uint32_t key) const {
+        if (XT == DT_U8 && counts) return uint64_t(key) << 34;
+        const double v = XT == DT_U8 ? ln[key] : double(Elem<XT>::value(key));
+        const double d = (v - m) * inv;
+        if (key == top) return uint64_t(1) << 42;                    // of +inf too
+        return key > 0 && d >= -double(kNats) ? exp_weight(d) : 0;
+    }
+    // the least weight that min_p leaves
+    __device__ __forceinline__ uint64_t least(double min_p) const {
+        return uint64_t(__builtin_ceil(min_p * one()));
+    }
+};
+
+// Only as many classes stay as start below this sum of the better ones' weights; the sums are
+// whole, so they are below p * sum iff they are below the next whole number.
+__device__ __forceinline__ uint64_t share(double p, uint64_t sum) {
+    if (p >= 1.0) return ~uint64_t(0);
+    const double s = __builtin_ceil(p * double(sum));
+    return s >= 1.0 ? uint64_t(s) : 1;                 // the best class always stays
+}
+
+// The class is the first whose running sum is larger than this.
+__device__ __forceinline__ uint64_t target(float u, uint64_t sum) {
+    const float most = 0.99999994f;                    // 1 - 2^-24
+    u = u > 0.0f ? (u < most ? u : most) : 0.0f;       // NaN: 0
+    return uint64_t(double(u) * double(sum));
+}
+
+__device__ __forceinline__ void fill_ln(double *ln) {
+    for (int i = threadIdx.x; i < 256; i += blockDim.x) ln[i] = log(double(i));
+    __syncthreads();
+}
+
+// ---- one lane a row ---------------------------------------------------------------------
+
+template <dt_dtype XT, int CP>
+__global__ void __launch_bounds__(256) sample_lanes(SampleArgs a) {
+    using O = Order<XT>;
+    __shared__ double ln[XT == DT_U8 ? 256 : 1];
+    if constexpr (XT == DT_U8) fill_ln(ln);
+    const int64_t row = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (row >= a.in.n) return;
+    const int n = a.in.classes;
+    typename Elem<XT>::Raw e[CP];
+    load_row<XT, CP>(a.in.x, row, a.in.ld, n, a.in.align, e);
+    const Settings set = settings_of<XT>(a, row);
+    typename O::T v[CP], first = 0;
+#pragma unroll
+    for (int i = 0; i < CP; ++i) {
+        v[i] = i < n ? O::make(Elem<XT>::key(e[i]), i) : 0;
+        first = v[i] > first ? v[i] : first;
+    }
+    if (O::key(first) == 0) {
+        a.labels[row] = -1;
+        return;
+    }
+    const Weights<XT> weight(set, O::key(first), ln);
+    const uint64_t least = weight.least(set.min_p);
+    typename O::T cut = 0;                 // classes from here on stay, in their order
+    uint64_t sum = 0;
+    if (set.k < n || set.p < 1.0) {
+        sort_registers<CP>(v);
+        uint64_t all = 0;
+#pragma unroll
+        for (int i = 0; i < CP; ++i)
+            if (i < set.k) all += weight(O::key(v[i]));
+        const uint64_t end = share(set.p, all);
+        uint64_t before = 0;
+#pragma unroll
+        for (int i = 0; i < CP; ++i)
+            if (i < set.k && before < end) {
+                const uint64_t w = weight(O::key(v[i]));
+                cut = v[i];
+                before += w;
+                if (w >= least) sum += w;
+            }
+#pragma unroll
+        for (int i = 0; i < CP; ++i) v[i] = i < n ? O::make(Elem<XT>::key(e[i]), i) : 0;
+    } else {
+#pragma unroll
+        for (int i = 0; i < CP; ++i) {
+            const uint64_t w = weight(O::key(v[i]));
+            if (w >= least) sum += w;
+        }
+    }
+    const uint64_t goal = target(a.u[row], sum);
+    uint64_t upto = 0;
+    int label = -1;
+#pragma unroll
+    for (int i = 0; i < CP; ++i) {
+        const uint64_t w = weight(O::key(v[i]));
+        if (v[i] >= cut && w >= least) upto += w;
+        if (label < 0 && upto > goal) label = i;
+    }
+    a.labels[row] = label;
+}
+
+// ---- a team a row -----------------------------------------------------------------------
+
+constexpr int bins_of(int waves) { return waves == 1 ? 256 : 1024; }
+
+template <int WAVES>
+struct Space {
+    Collected c;
+    uint64_t weight[DS_MAX_TOP];
+    uint64_t mass[bins_of(WAVES)];
+    uint32_t number[bins_of(WAVES)];
+    uint64_t part[16];
+    // answers that one thread finds and all read
+    int bin, index;
+    uint64_t found, before;
+};
+
+// A class's place on a scale of kNats / kBins steps below the best: the larger the score the
+// lower the bin (each step of the computation keeps the order); kBins for weight 0.
+template <dt_dtype XT, int WAVES>
+struct Scale {
+    uint32_t top;
+    float m, step;
+    __device__ __forceinline__ Scale(const Weights<XT> &w)
+        : top(w.top), m(Elem<XT>::value(w.top)), step(float(w.inv * (bins_of(WAVES) / kNats))) {}
+    __device__ __forceinline__ int bin(uint32_t key) const {
+        constexpr int n = bins_of(WAVES);
+        if (key == top) return 0;
+        const float d = (m - Elem<XT>::value(key)) * step;
+        return key > 0 && d < float(n) ? int(d) : n;
+    }
+};
+
+// Where the best-first order of a row ends: at the q-th class (BY_WEIGHT false) or at the class
+// that makes the sum of weights reach q.  In: the histogram in s.  Out: comp() of the last
+// class that stays, and in s.found the weight of all that stay (if not BY_WEIGHT).
+template <bool BY_WEIGHT, dt_dtype XT, int WAVES>
+__device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &row, const Weights<XT> &weight,
+                           const Scale<XT, WAVES> &scale, uint64_t q, Space<WAVES> &s) {
+    constexpr int kBins = bins_of(WAVES), kEach = kBins / Team<WAVES>::kThreads;
+    static_assert(kEach >= 1, "");
+    // the bin in which it lies
+    uint64_t w = 0, all_w;
+    int n = 0, all_n;
+    if (t.thread == 0) s.bin = -1;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        w += s.mass[t.thread * kEach + i];
+        n += int(s.number[t.thread * kEach + i]);
+    }
+    uint64_t w0 = t.before(w, &all_w);
+    int n0 = t.before(n, &all_n);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int b = t.thread * kEach + i;
+        const uint64_t bw = s.mass[b];
+        const int bn = int(s.number[b]);
+        const bool here = BY_WEIGHT ? (w0 < q && q <= w0 + bw)
+                                    : (uint64_t(n0) < q && q <= uint64_t(n0) + uint64_t(bn));
+        if (here) {
+            s.bin = b;
+            s.before = w0;
+            s.index = n0;
+        }
+        w0 += bw;
+        n0 += bn;
+    }
+    t.sync();
+    const int bin = s.bin;
+    if (bin < 0) {                           // beyond every class with a weight
+        if (t.thread == 0) s.found = all_w;
+        t.sync();
+        return 0;
+    }
+    const uint64_t before_w = s.before;
+    const uint64_t rest = BY_WEIGHT ? q - before_w : q - uint64_t(s.index);
+    const int members = int(s.number[bin]);
+    t.sync();
+    if (members <= kCap) {
+        if (t.thread == 0) s.c.count = 0;
+        t.sync();
+        row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int c) {
+            const uint32_t key = Elem<XT>::key(e);
+            if (scale.bin(key) == bin) s.c.list[atomicAdd(&s.c.count, 1)] = comp(key, c);
+        });
+        t.sync();
+        sort_list(t, s.c.list, members);
+        uint64_t run = 0;
+        for (int i0 = 0; i0 < members; i0 += t.kThreads) {
+            const int i = i0 + t.thread;
+            const uint64_t wi = i < members ? weight(comp_key(s.c.list[i])) : 0;
+            uint64_t all;
+            const uint64_t b = run + t.before(wi, &all);
+            const bool here = BY_WEIGHT ? (b < rest && rest <= b + wi) : uint64_t(i) + 1 == rest;
+            if (i < members && here) {
+                s.index = i;
+                s.found = before_w + b + wi;
+            }
+            run += all;
+        }
+        t.sync();
+        return s.c.list[s.index];
+    }
+    // Too many to collect: the key at which it lies, by halving, and the place among the
+    // classes of that key.
+    auto from = [&](uint32_t least, int *count) {
+        uint64_t sum = 0;
+        int k = 0;
+        row.template each<1>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
+            const uint32_t key = Elem<XT>::key(e);
+            if (key >= least && scale.bin(key) == bin) {
+                sum += weight(key);
+                ++k;
+            }
+        });
+        *count = t.reduce(k, Sum());
+        return t.reduce(sum, Sum());
+    };
+    uint32_t lo = 1, hi = weight.top + 1;      // from(lo) >= rest > from(hi)
+    int count;
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + ((hi - lo) >> 1);
+        const uint64_t sum = from(mid, &count);
+        if ((BY_WEIGHT ? sum : uint64_t(count)) >= rest)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    const uint64_t above = hi > weight.top ? (count = 0, uint64_t(0)) : from(hi, &count);
+    const uint64_t one = weight(lo);
+    const uint64_t nth = BY_WEIGHT ? (rest - above + one - 1) / one : rest - uint64_t(count);
+    const int c = nth_equal<XT>(t, row, lo, int(nth), &s.index);
+    t.sync();
+    if (t.thread == 0) s.found = before_w + above + nth * one;
+    t.sync();
+    return comp(lo, c);
+}
+
+// The drawn class among s.c.best[0 .. k), which are in order.
+template <dt_dtype XT, int WAVES>
+__device__ __forceinline__ int draw_of_few(const Team<WAVES> &t, const Weights<XT> &weight, const Settings &set,
+                           int k, float u, Space<WAVES> &s) {
+    for (int j = t.thread; j < DS_MAX_TOP; j += t.kThreads)
+        s.weight[j] = j < k ? weight(comp_key(s.c.best[j])) : 0;
+    t.sync();
+    if (t.wave == 0) {
+        constexpr int kEach = DS_MAX_TOP / 64;
+        uint64_t w[kEach], mine = 0, all;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            w[i] = s.weight[t.lane * kEach + i];
+            mine += w[i];
+        }
+        uint64_t before = wave_before(mine, t.lane, &all);
+        const uint64_t end = share(set.p, all), least = weight.least(set.min_p);
+        int stay = 0;
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = t.lane * kEach + i;
+            if (j < k && before < end && w[i] >= least) {
+                ++stay;                      // they are the first ones: both limits are ordered
+                sum += w[i];
+            }
+            before += w[i];
+        }
+        stay = wave_reduce(stay, Sum());
+        sum = wave_reduce(sum, Sum());
+        if (t.lane == 0) {
+            s.index = stay;
+            s.found = target(u, sum);
+        }
+    }
+    t.sync();
+    const int stay = s.index;
+    const uint64_t goal = s.found;
+    for (int j = t.thread; j < stay; j += t.kThreads) {
+        const int c = comp_class(s.c.best[j]);
+        uint64_t upto = 0;
+#pragma unroll 8
+        for (int i = 0; i < stay; ++i)
+            upto += comp_class(s.c.best[i]) <= c ? s.weight[i] : 0;
+        if (upto > goal && upto - s.weight[j] <= goal) s.bin = c;
+    }
+    t.sync();
+    return s.bin;
+}
+
+// The drawn class among all that stay: those from `cut` on, of weight `least` or more.
+template <dt_dtype XT, int WAVES>
+__device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &row, const Weights<XT> &weight,
+                           uint64_t cut, uint64_t least, float u, Space<WAVES> &s) {
+    auto staying = [&](auto e, int c) {
+        const uint32_t key = Elem<XT>::key(e);
+        if (comp(key, c) < cut) return uint64_t(0);
+        const uint64_t w = weight(key);
+        return w >= least ? w : uint64_t(0);
+    };
+    // each wavefront sums a stretch of the row
+    const int per = (row.vecs + WAVES - 1) / WAVES;
+    auto start = [&](int w) { return w * per < row.vecs ? w * per : row.vecs; };
+    uint64_t sum = 0;
+    row.template each<1>(start(t.wave), start(t.wave + 1), t.lane, 64,
+                         [&](auto e, int c) { sum += staying(e, c); });
+    sum = wave_reduce(sum, Sum());
+    uint64_t all = 0;
+    if constexpr (WAVES == 1) {
+        all = sum;
+    } else {
+        if (t.lane == 0) s.part[t.wave] = sum;
+        t.sync();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) all += s.part[w];
+    }
+    const uint64_t goal = target(u, all);
+    // the stretch, then the vector, then the class at which the sum passes the goal
+    uint64_t run = 0;
+    int which = 0;
+    if constexpr (WAVES > 1) {
+        while (which < WAVES - 1 && run + s.part[which] <= goal) run += s.part[which++];
+    }
+    const int hi = start(which + 1);
+    for (int v0 = start(which); v0 < hi && run <= goal; v0 += t.kThreads) {
+        const int v = v0 + t.thread;
+        u32x4 a = {0u, 0u, 0u, 0u};
+        uint64_t mine = 0, tile;
+        if (v < hi) {
+            a = row.load(v);
+            row.visit(a, v, [&](auto e, int c) { mine += staying(e, c); });
+        }
+        uint64_t upto = run + t.before(mine, &tile);
+        if (upto <= goal && goal < upto + mine)
+            row.visit(a, v, [&](auto e, int c) {
+                const uint64_t w = staying(e, c);
+                if (upto <= goal && goal < upto + w) s.bin = c;
+                upto += w;
+            });
+        run += tile;
+    }
+    t.sync();
+    return s.bin;
+}
+
+template <dt_dtype XT, int WAVES>
+__global__ void __launch_bounds__(WAVES == 16 ? 1024 : 256) sample_teams(SampleArgs a) {
+    constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
+    __shared__ Space<WAVES> space[kTeams];
+    __shared__ uint64_t box[WAVES];
+    __shared__ double ln[XT == DT_U8 ? 256 : 1];
+    if constexpr (XT == DT_U8) fill_ln(ln);
+    const int which = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const int thread = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const Team<WAVES> t{thread, thread & 63, thread >> 6, box};
+    Space<WAVES> &s = space[which];
+    const int n = a.in.classes;
+    for (int64_t r = int64_t(blockIdx.x) * kTeams + which; r < a.in.n;
+         r += int64_t(gridDim.x) * kTeams) {
+        const Row<XT> row(a.in.x, r, a.in.ld, n);
+        const Settings set = settings_of<XT>(a, r);
+        const float u = a.u[r];
+        uint32_t mine = 0;
+        row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
+            const uint32_t key = Elem<XT>::key(e);
+            mine = key > mine ? key : mine;
+        });
+        const uint32_t top = t.reduce(mine, Max());
+        int label = -1;
+        if (top > 0) {
+            const Weights<XT> weight(set, top, ln);
+            if (set.k <= DS_MAX_TOP && set.k < n) {
+                const int k = best_of_row<XT>(t, row, set.k, mine, top, s.c, [](auto, uint32_t) {});
+                label = draw_of_few(t, weight, set, k, u, s);
+            } else {
+                uint64_t cut = 0;
+                if (set.k < n || set.p < 1.0) {
+                    const Scale<XT, WAVES> scale(weight);
+                    constexpr int kBins = bins_of(WAVES);
+                    for (int b = t.thread; b < kBins; b += t.kThreads) {
+                        s.mass[b] = 0;
+                        s.number[b] = 0;
+                    }
+                    t.sync();
+                    row.template each<1>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
+                        const uint32_t key = Elem<XT>::key(e);
+                        const int b = scale.bin(key);
+                        if (b < kBins) {
+                            atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[b]),
+                                      static_cast<unsigned long long>(weight(key)));
+                            atomicAdd(&s.number[b], 1u);
+                        }
+                    });
+                    t.sync();
+                    // by number first: of the rest's weight, top-p's share
+                    cut = end_of<false, XT, WAVES>(
+                        t, row, weight, scale, set.k < n ? uint64_t(set.k) : ~uint64_t(0), s);
+                    const uint64_t all = s.found;
+                    t.sync();
+                    if (set.p < 1.0)
+                        cut = end_of<true, XT, WAVES>(t, row, weight, scale, share(set.p, all), s);
+                }
+                label = draw_of_row(t, row, weight, cut, weight.least(set.min_p), u, s);
+            }
+        }
+        if (t.thread == 0) a.labels[r] = label;
+        t.sync();
+    }
+}
+
+template <dt_dtype XT, int WAVES>
+void run_teams(const SampleArgs &a, hipStream_t stream) {
+    constexpr int kTeams = WAVES == 1 ? 4 : 1;
+    const int64_t blocks = (a.in.n + kTeams - 1) / kTeams;
+    sample_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 16 ? 1024 : 256,
+                              0, stream>>>(a);
+}
+
+template <dt_dtype XT>
+void run(const SampleArgs &a, hipStream_t stream) {
+    const int c = a.in.classes;
+    if (c <= kLaneClasses) {
+        const unsigned blocks = unsigned((a.in.n + 255) / 256);
+        if (c <= 8) sample_lanes<XT, 8><<<blocks, 256, 0, stream>>>(a);
+        else if (c <= 16) sample_lanes<XT, 16><<<blocks, 256, 0, stream>>>(a);
+        else if (c <= 32) sample_lanes<XT, 32><<<blocks, 256, 0, stream>>>(a);
+        else sample_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
+    } else if (c <= kCap) {
+        run_teams<XT, 1>(a, stream);       // everything can be collected
+    } else if (c <= 8192) {
+        run_teams<XT, 4>(a, stream);
+    } else {
+        run_teams<XT, 16>(a, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_sample(const SampleArgs &a, dt_dtype type, hipStream_t stream) {
+    switch (type) {
+        case DT_F32: run<DT_F32>(a, stream); break;
+        case DT_F16: run<DT_F16>(a, stream); break;
+        case DT_BF16: run<DT_BF16>(a, stream); break;
+        case DT_U8: run<DT_U8>(a, stream); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dscores

@@ -1,0 +1,134 @@
+// The k best classes of each row and the row's log-sum-exp (ds_top_scores).
+#include "scores.hpp"
+#include "scores_lanes.hpp"
+#include "scores_select.hpp"
+
+namespace dscores {
+namespace {
+
+template <dt_dtype XT>
+__device__ __forceinline__ float log_sum(uint32_t top, float sum) {
+    if (top == 0) return -__builtin_inff();
+    if constexpr (XT == DT_U8) return logf(sum);           // ln of the votes
+    return Elem<XT>::value(top) + logf(sum);
+}
+
+// One lane a row.
+template <dt_dtype XT, int CP>
+__global__ void __launch_bounds__(256) top_lanes(TopArgs a) {
+    using O = Order<XT>;
+    const int64_t row = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (row >= a.in.n) return;
+    typename Elem<XT>::Raw e[CP];
+    load_row<XT, CP>(a.in.x, row, a.in.ld, a.in.classes, a.in.align, e);
+    typename O::T v[CP];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < CP; ++i) {
+        const uint32_t key = i < a.in.classes ? Elem<XT>::key(e[i]) : 0u;
+        top = key > top ? key : top;
+        v[i] = i < a.in.classes ? O::make(key, i) : 0;
+    }
+    const float m = Elem<XT>::value(top);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < CP; ++i) {
+        const uint32_t key = O::key(v[i]);
+        if constexpr (XT == DT_U8)
+            sum += float(key);
+        else if (key > 0)
+            sum += key == top ? 1.0f : exp_neg(Elem<XT>::value(key) - m);
+    }
+    a.lse[row] = log_sum<XT>(top, sum);
+    sort_registers<CP>(v);
+    float *values = a.values + row * a.k;
+    int32_t *index = a.index + row * a.k;
+#pragma unroll
+    for (int i = 0; i < CP; ++i)
+        if (i < a.k) {
+            const uint32_t key = O::key(v[i]);
+            values[i] = key > 0 ? Elem<XT>::value(key) : -__builtin_inff();
+            index[i] = key > 0 ? O::cls(v[i]) : -1;
+        }
+}
+
+// A team a row.
+template <dt_dtype XT, int WAVES>
+__global__ void __launch_bounds__(WAVES == 16 ? 1024 : 256) top_teams(TopArgs a) {
+    constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
+    __shared__ Collected space[kTeams];
+    __shared__ uint64_t box[WAVES];
+    const int which = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const int thread = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const Team<WAVES> t{thread, thread & 63, thread >> 6, box};
+    Collected &s = space[which];
+    for (int64_t r = int64_t(blockIdx.x) * kTeams + which; r < a.in.n;
+         r += int64_t(gridDim.x) * kTeams) {
+        const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
+        uint32_t mine = 0;
+        row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
+            const uint32_t key = Elem<XT>::key(e);
+            mine = key > mine ? key : mine;
+        });
+        const uint32_t top = t.reduce(mine, Max());
+        int found = 0;
+        float sum = 0.0f;
+        if (top > 0) {
+            const float m = Elem<XT>::value(top);
+            found = best_of_row<XT>(t, row, a.k, mine, top, s, [&](auto e, uint32_t key) {
+                if constexpr (XT == DT_U8)
+                    sum += float(key);
+                else if (key > 0)
+                    sum += key == top ? 1.0f : exp_neg(Elem<XT>::wide(e) - m);
+            });
+            sum = t.reduce(sum, Sum());
+        }
+        if (t.thread == 0) a.lse[r] = log_sum<XT>(top, sum);
+        for (int j = t.thread; j < a.k; j += t.kThreads) {
+            const uint32_t key = j < found ? comp_key(s.best[j]) : 0u;
+            a.values[r * a.k + j] = key > 0 ? Elem<XT>::value(key) : -__builtin_inff();
+            a.index[r * a.k + j] = key > 0 ? comp_class(s.best[j]) : -1;
+        }
+        t.sync();
+    }
+}
+
+template <dt_dtype XT, int WAVES>
+void run_teams(const TopArgs &a, hipStream_t stream) {
+    constexpr int kTeams = WAVES == 1 ? 4 : 1;
+    const int64_t blocks = (a.in.n + kTeams - 1) / kTeams;
+    top_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 16 ? 1024 : 256, 0,
+                           stream>>>(a);
+}
+
+template <dt_dtype XT>
+void run(const TopArgs &a, hipStream_t stream) {
+    const int c = a.in.classes;
+    if (c <= kLaneClasses) {
+        const unsigned blocks = unsigned((a.in.n + 255) / 256);
+        if (c <= 8) top_lanes<XT, 8><<<blocks, 256, 0, stream>>>(a);
+        else if (c <= 16) top_lanes<XT, 16><<<blocks, 256, 0, stream>>>(a);
+        else if (c <= 32) top_lanes<XT, 32><<<blocks, 256, 0, stream>>>(a);
+        else top_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
+    } else if (c <= kCap) {
+        run_teams<XT, 1>(a, stream);       // everything can be collected
+    } else if (c <= 8192 && a.k <= 64) {
+        run_teams<XT, 4>(a, stream);
+    } else {
+        run_teams<XT, 16>(a, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_top(const TopArgs &a, dt_dtype type, hipStream_t stream) {
+    switch (type) {
+        case DT_F32: run<DT_F32>(a, stream); break;
+        case DT_F16: run<DT_F16>(a, stream); break;
+        case DT_BF16: run<DT_BF16>(a, stream); break;
+        case DT_U8: run<DT_U8>(a, stream); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dscores
