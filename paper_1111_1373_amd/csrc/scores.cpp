@@ -54,7 +54,7 @@ dt_status teacher_of(const float *values, const int32_t *index, int32_t k, float
     if (k < 1 || k > DS_MAX_TOP) return fail(DT_ERR_INVALID_ARG, "k must be 1 .. 256");
     if (!(temperature > 0.0f && temperature <= 3.402823466e38f))
         return fail(DT_ERR_INVALID_ARG, "temperature must be positive and finite");
-    if (!(1.0f / temperature <= 3.402823466e38f))
+    if (!(1.5f / temperature <= 3.402823466e38f))      // log2 e over it is used
         return fail(DT_ERR_INVALID_ARG, "temperature is too small");
     if (a->in.n > 0 && (!values || !index)) return fail(DT_ERR_INVALID_ARG, "null teacher");
     if (misaligned(values, 4) || misaligned(index, 4))

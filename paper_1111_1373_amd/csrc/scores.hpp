@@ -9,8 +9,9 @@
 
 namespace dscores {
 
-// Rows of few classes are worked on by one lane each, others by teams of 1, 4 or 16 wavefronts.
+// Rows of few classes are worked on by one lane each, others by teams of 1, 4 or 8 wavefronts.
 constexpr int kLaneClasses = 64;
+constexpr int kBigTeam = 8;
 
 struct RowArgs {
     const void *x;

@@ -13,84 +13,186 @@ namespace dscores {
 
 // ---- elements ---------------------------------------------------------------------------
 //
-// key() maps an element to an unsigned number of the same order, 0 for what is never chosen
-// (-inf, NaN, no votes, and places outside the row); value() maps it back to the score.
+// rank() maps an element to an unsigned number of the order of scores, NaN of either sign and -inf
+// at the bottom (up to kNone): the bits of a float, complemented below zero and with the sign bit
+// set above, are in order already, and adding the number of positive NaNs turns these round to
+// the bottom.  It takes four operations, on two elements at a time for the 16-bit types, and is
+// what walks over long rows look at.  The two zeros are neighbours.
+//
+// key() is the rank with the zeros made equal and 0 for what is never chosen (also the places
+// outside a row); value() maps a key back to the score.
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <dt_dtype XT>
 struct Elem;
 
-__device__ __forceinline__ uint32_t float_key(float f) {
-    const uint32_t b = __float_as_uint(f + 0.0f);                    // -0 becomes +0
-    const uint32_t o = b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
-    return f > -__builtin_inff() ? o : 0u;                           // false for NaN
-}
-
-__device__ __forceinline__ float key_float(uint32_t k) {
-    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
-}
+// Ranks of float types: TURN positive NaNs, ranks of BITS bits.
+template <uint32_t TURN, int BITS>
+struct FloatRanks {
+    static constexpr uint32_t kMask = BITS == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+    static constexpr uint32_t kSign = 1u << (BITS - 1);
+    static constexpr uint32_t kNone = 2 * TURN;                     // -inf
+    static constexpr uint32_t kZero = kSign + TURN;                 // +0; -0 is one below
+    static __device__ __forceinline__ uint32_t rank_of_bits(uint32_t b) {
+        const uint32_t o = b & kSign ? ~b : b | kSign;
+        return (o + TURN) & kMask;
+    }
+    static __device__ __forceinline__ uint32_t bits_of_key(uint32_t k) {
+        const uint32_t o = (k - TURN) & kMask;
+        return o & kSign ? o ^ kSign : ~o & kMask;
+    }
+    static __device__ __forceinline__ uint32_t key_of_rank(uint32_t r) {
+        return r <= kNone ? 0u : r == kZero - 1 ? kZero : r;
+    }
+    // the lowest rank whose key is at least this rank's
+    static __device__ __forceinline__ uint32_t from_rank(uint32_t r) { return r == kZero ? r - 1 : r; }
+};
 
 template <>
-struct Elem<DT_F32> {
+struct Elem<DT_F32> : FloatRanks<0x007FFFFFu, 32> {
     using Raw = uint32_t;
-    static constexpr int kBytes = 4, kKeyBits = 32;
+    static constexpr int kBytes = 4;
     static __device__ __forceinline__ float wide(Raw r) { return __uint_as_float(r); }
-    static __device__ __forceinline__ uint32_t key(Raw r) { return float_key(wide(r)); }
-    static __device__ __forceinline__ float value(uint32_t k) { return key_float(k); }
+    static __device__ __forceinline__ uint32_t rank(Raw r) { return rank_of_bits(r); }
+    static __device__ __forceinline__ uint32_t key(Raw r) { return key_of_rank(rank(r)); }
+    static __device__ __forceinline__ float value(uint32_t k) { return __uint_as_float(bits_of_key(k)); }
     static __device__ __forceinline__ Raw narrow(float f) { return __float_as_uint(f); }
 };
 
-// The 16-bit types' keys have 16 bits: the ordered bits of the element itself.
-__device__ __forceinline__ uint32_t half_order(uint32_t b) {
-    return (b & 0x8000u) ? (~b & 0xFFFFu) : (b | 0x8000u);
-}
-
 template <>
-struct Elem<DT_F16> {
+struct Elem<DT_F16> : FloatRanks<0x03FFu, 16> {
     using Raw = uint16_t;
-    static constexpr int kBytes = 2, kKeyBits = 16;
+    static constexpr int kBytes = 2;
     static __device__ __forceinline__ float wide(Raw r) {
         return float(__builtin_bit_cast(_Float16, r));
     }
-    static __device__ __forceinline__ uint32_t key(Raw r) {
-        const uint32_t b = r == 0x8000u ? 0u : r;
-        // -inf, and NaN of either sign
-        return (b == 0xFC00u || (b & 0x7FFFu) > 0x7C00u) ? 0u : half_order(b);
-    }
-    static __device__ __forceinline__ float value(uint32_t k) {
-        return wide(Raw(k & 0x8000u ? k ^ 0x8000u : ~k & 0xFFFFu));
-    }
+    static __device__ __forceinline__ uint32_t rank(Raw r) { return rank_of_bits(r); }
+    static __device__ __forceinline__ uint32_t key(Raw r) { return key_of_rank(rank(r)); }
+    static __device__ __forceinline__ float value(uint32_t k) { return wide(Raw(bits_of_key(k))); }
     static __device__ __forceinline__ Raw narrow(float f) {
         return __builtin_bit_cast(Raw, _Float16(f));
     }
 };
 
 template <>
-struct Elem<DT_BF16> {
+struct Elem<DT_BF16> : FloatRanks<0x007Fu, 16> {
     using Raw = uint16_t;
-    static constexpr int kBytes = 2, kKeyBits = 16;
+    static constexpr int kBytes = 2;
     static __device__ __forceinline__ float wide(Raw r) { return __uint_as_float(uint32_t(r) << 16); }
-    static __device__ __forceinline__ uint32_t key(Raw r) {
-        const uint32_t b = r == 0x8000u ? 0u : r;
-        return (b == 0xFF80u || (b & 0x7FFFu) > 0x7F80u) ? 0u : half_order(b);
-    }
-    static __device__ __forceinline__ float value(uint32_t k) {
-        return wide(Raw(k & 0x8000u ? k ^ 0x8000u : ~k & 0xFFFFu));
-    }
-    // to the nearest, ties to even; a NaN keeps its place
+    static __device__ __forceinline__ uint32_t rank(Raw r) { return rank_of_bits(r); }
+    static __device__ __forceinline__ uint32_t key(Raw r) { return key_of_rank(rank(r)); }
+    static __device__ __forceinline__ float value(uint32_t k) { return wide(Raw(bits_of_key(k))); }
+    // to the nearest, ties to even
     static __device__ __forceinline__ Raw narrow(float f) {
-        const uint32_t b = __float_as_uint(f);
-        const uint32_t r = (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
-        return f != f ? Raw(0x7FC0u) : Raw(r);
+        return __builtin_bit_cast(Raw, __bf16(f));
     }
 };
 
+// Votes: the number itself, none at the bottom.
 template <>
 struct Elem<DT_U8> {
     using Raw = uint8_t;
-    static constexpr int kBytes = 1, kKeyBits = 8;
+    static constexpr int kBytes = 1;
+    static constexpr uint32_t kNone = 0;
     static __device__ __forceinline__ float wide(Raw r) { return logf(float(r)); }
+    static __device__ __forceinline__ uint32_t rank(Raw r) { return r; }
     static __device__ __forceinline__ uint32_t key(Raw r) { return r; }
+    static __device__ __forceinline__ uint32_t key_of_rank(uint32_t r) { return r; }
+    static __device__ __forceinline__ uint32_t from_rank(uint32_t r) { return r; }
     static __device__ __forceinline__ float value(uint32_t k) { return logf(float(k)); }
+};
+
+// The ranks of a vector of 16 bytes, and a running maximum of them.
+template <dt_dtype XT>
+struct Ranks {
+    using E = Elem<XT>;
+    // of the four words of a vector: ranks of its elements, in pairs of 16 bits for narrow types
+    static constexpr int kWords = XT == DT_U8 ? 8 : 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ explicit Ranks(const u32x4 &a) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (XT == DT_F32) {
+                w[i] = E::rank(a[i]);
+            } else if constexpr (XT == DT_U8) {
+                w[i] = a[i] & 0x00FF00FFu;
+                w[4 + i] = (a[i] >> 8) & 0x00FF00FFu;
+            } else {
+                // all ones in the halves below zero, the sign bit in the others (in whole words:
+                // of packed 16-bit shifts of a vector's four words the compiler made one)
+                const u16x2 turn = {uint16_t(E::kNone / 2), uint16_t(E::kNone / 2)};
+                const uint32_t sign = a[i] & 0x80008000u;
+                const uint32_t flip = (sign - (sign >> 15)) | 0x80008000u;
+                w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2, a[i] ^ flip) + turn);
+            }
+        }
+    }
+    // A running maximum, in the words' form
+    struct Max {
+        uint32_t v = 0;
+        __device__ __forceinline__ void add(const Ranks &r) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                if constexpr (XT == DT_F32)
+                    v = r.w[i] > v ? r.w[i] : v;
+                else
+                    v = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
+                            __builtin_bit_cast(u16x2, r.w[i]), __builtin_bit_cast(u16x2, v)));
+            }
+        }
+        __device__ __forceinline__ uint32_t rank() const {
+            if constexpr (XT == DT_F32) return v;
+            return (v & 0xFFFFu) > (v >> 16) ? v & 0xFFFFu : v >> 16;
+        }
+    };
+};
+
+// Whether any element of a vector may reach a bound: of the float types the largest of the widened
+// elements, three operands an instruction, which costs half an operation an element where the
+// ranks cost three.  A NaN may hide the largest or be it: then the answer is yes, and the
+// elements' ranks tell.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+template <dt_dtype XT>
+struct Filter {
+    using E = Elem<XT>;
+    uint32_t least;        // rank, > kNone
+    float bound;
+    __device__ __forceinline__ explicit Filter(uint32_t least_rank) : least(least_rank) {
+        if constexpr (XT != DT_U8) bound = E::value(E::key_of_rank(least));
+    }
+    __device__ __forceinline__ bool any(const u32x4 &a) const {
+        if constexpr (XT == DT_U8) {
+            // what a number has above least - 1, or nothing
+            const u16x2 below = {uint16_t(least - 1), uint16_t(least - 1)};
+            uint32_t some = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t w = (i < 4 ? a[i & 3] : a[i & 3] >> 8) & 0x00FF00FFu;
+                some |= __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(
+                            __builtin_bit_cast(u16x2, w), below));
+            }
+            return some != 0;
+        } else {
+            constexpr int kVec = 16 / E::kBytes, kPerWord = 4 / E::kBytes;
+            float x[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                x[i] = E::wide(typename E::Raw(a[i / kPerWord] >> (8 * E::kBytes * (i % kPerWord))));
+            float m = max3(x[0], x[1], x[2]);
+#pragma unroll
+            for (int i = 3; i + 1 < kVec; i += 2) m = max3(m, x[i], x[i + 1]);
+            if constexpr (kVec % 2 == 0) m = max3(m, x[kVec - 1], x[kVec - 1]);
+            return !(m < bound);
+        }
+    }
 };
 
 // ---- rows -------------------------------------------------------------------------------
@@ -98,8 +200,6 @@ struct Elem<DT_U8> {
 // A row is read in aligned 16-byte vectors.  The first and the last may reach beyond the row:
 // of those only the row's own elements are read, one by one.  Vector v holds the classes
 // first(v) .. first(v) + kVec - 1.
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <dt_dtype XT>
 struct Row {
@@ -223,12 +323,33 @@ struct Sum {
     __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
 };
 
-// Over groups of `width` neighbouring lanes (a power of two).
-template <class T, class Op>
-__device__ __forceinline__ T wave_reduce(T v, Op op, int width = 64) {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1)
-        if (m < width) v = op(v, xor_lane(v, m));
+// A lane's partner in a reduction: by data-parallel moves within rows of 16 lanes, where a
+// mirrored lane holds the same as the xor partner once the steps below it are done.
+template <int STEP, class T>
+__device__ __forceinline__ T partner(T v) {
+    if constexpr (STEP >= 16) {
+        return xor_lane(v, STEP);
+    } else if constexpr (sizeof(T) == 8) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = partner<STEP>(uint32_t(b)), hi = partner<STEP>(uint32_t(b >> 32));
+        return __builtin_bit_cast(T, uint64_t(hi) << 32 | lo);
+    } else {
+        // quad_perm [1,0,3,2], quad_perm [2,3,0,1], row_half_mirror, row_mirror
+        constexpr int kControl = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : STEP == 4 ? 0x141 : 0x140;
+        const int b = __builtin_bit_cast(int, v);
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(b, b, kControl, 0xF, 0xF, true));
+    }
+}
+
+// Over groups of WIDTH neighbouring lanes (a power of two); every lane gets the result.
+template <int WIDTH = 64, class T, class Op>
+__device__ __forceinline__ T wave_reduce(T v, Op op) {
+    if constexpr (WIDTH > 1) v = op(v, partner<1>(v));
+    if constexpr (WIDTH > 2) v = op(v, partner<2>(v));
+    if constexpr (WIDTH > 4) v = op(v, partner<4>(v));
+    if constexpr (WIDTH > 8) v = op(v, partner<8>(v));
+    if constexpr (WIDTH > 16) v = op(v, partner<16>(v));
+    if constexpr (WIDTH > 32) v = op(v, partner<32>(v));
     return v;
 }
 

@@ -33,7 +33,7 @@ struct Group {
     }
     template <class Op>
     __device__ __forceinline__ float reduce(float v, Op op) const {
-        v = wave_reduce(v, op, G < 64 ? G : 64);
+        v = wave_reduce<(G < 64 ? G : 64)>(v, op);
         if constexpr (G > 64) {
             sync();
             if ((thread & 63) == 0) box[thread >> 6] = v;
@@ -51,41 +51,52 @@ struct MaxNum {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
+// e^((x - m) / t) as 2^((x - m) log2 e / t), c = log2 e / t.  The difference comes first, so that a
+// common part of all scores (or a whole row of a type's lowest value) costs nothing; the product's
+// rounding is at most 1.5 steps of the exponent, which only small terms have large.  m = -inf: then x
+// is too, or NaN.
+__device__ __forceinline__ float power(float x, float m, float c) {
+    return __builtin_amdgcn_exp2f((x - m) * c);
+}
+__device__ __forceinline__ float finite(float m) { return m == -__builtin_inff() ? 0.0f : m; }
+
+constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+
 // The largest of some scores, and the sum of e^((x - largest) / t) over them.
 struct Stats {
     float m = -__builtin_inff(), s = 0.0f;
 
-    // x - m where m may be -inf (then x is too, or NaN)
-    static __device__ __forceinline__ float below(float x, float m) {
-        return x - (m == -__builtin_inff() ? 0.0f : m);
-    }
-    __device__ __forceinline__ void raise(float m1, float inv) {
+    __device__ __forceinline__ void raise(float m1, float c) {
         if (m1 > m) {
-            s *= exp_neg(below(m, m1) * inv);
+            s *= power(m, m1, c);
             m = m1;
         }
     }
-    __device__ __forceinline__ void add(float x, float inv) {
-        raise(x, inv);
-        s += exp_neg(below(x, m) * inv);
+    __device__ __forceinline__ void add(float x, float c) {
+        raise(x, c);
+        s += power(x, finite(m), c);
     }
     template <dt_dtype XT>
-    __device__ __forceinline__ void add(const Row<XT> &row, const u32x4 &a, float inv) {
+    __device__ __forceinline__ void add(const Row<XT> &row, const u32x4 &a, float c) {
         using E = Elem<XT>;
-        float x[Row<XT>::kVec], top = -__builtin_inff();
+        constexpr int kVec = Row<XT>::kVec;
+        float x[kVec];
 #pragma unroll
-        for (int i = 0; i < Row<XT>::kVec; ++i) {
-            x[i] = E::wide(row.at(a, i));
-            top = fmaxf(top, x[i]);
-        }
-        raise(top, inv);
-        const float base = m == -__builtin_inff() ? 0.0f : m;
+        for (int i = 0; i < kVec; ++i) x[i] = E::wide(row.at(a, i));
+        // (a NaN may be the largest here: `raise` passes over it, and the sum keeps it; one that
+        // hides a larger score from the maximum has made the sum a NaN as well)
+        float top = max3(x[0], x[1], x[2]);
 #pragma unroll
-        for (int i = 0; i < Row<XT>::kVec; ++i) s += exp_neg((x[i] - base) * inv);
+        for (int i = 3; i + 1 < kVec; i += 2) top = max3(top, x[i], x[i + 1]);
+        top = max3(top, x[kVec - 1], x[kVec - 1]);
+        raise(top, c);
+        const float base = finite(m);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) s += power(x[i], base, c);
     }
     template <class Gr>
-    __device__ __forceinline__ void join(const Gr &g, float inv) {
-        raise(g.reduce(m, MaxNum()), inv);
+    __device__ __forceinline__ void join(const Gr &g, float c) {
+        raise(g.reduce(m, MaxNum()), c);
         s = g.reduce(s, Sum());
     }
     // without any score above -inf (a NaN counts as one)
@@ -103,48 +114,46 @@ template <dt_dtype XT, int MODE, class Gr>
 __device__ __forceinline__ bool teach(const DistillArgs &a, const Gr &g, int threads, int64_t r,
                                       const Row<XT> &row, const Stats &st, const Entries &e,
                                       float *loss) {
+    const float c2 = kLog2E / a.temperature;
     const float inv = 1.0f / a.temperature;
     const float *values = a.values + r * a.k;
     const int32_t *index = a.index + r * a.k;
-    float top = -__builtin_inff(), any = 0.0f;
+    float top = -__builtin_inff();
     for (int j = g.thread; j < a.k; j += threads) {
         const float v = values[j];
         const int c = index[j];
         const bool in = c >= 0 && c < a.in.classes && v != -__builtin_inff();
         e.cls[j] = in ? c : -1;
         e.p[j] = v;
-        if (in) {
-            any = 1.0f;
-            top = fmaxf(top, v);
-        }
+        if (in) top = fmaxf(top, v);
     }
-    any = g.reduce(any, MaxNum());
     top = g.reduce(top, MaxNum());
     float sum = 0.0f;
     for (int j = g.thread; j < a.k; j += threads)
-        if (e.cls[j] >= 0) sum += exp_neg((e.p[j] - top) * inv);
+        if (e.cls[j] >= 0) sum += power(e.p[j], top, c2);
     sum = g.reduce(sum, Sum());
-    const float log_sum = logf(sum), log_s = MODE == kGradOnly ? 0.0f : logf(st.s);
+    const bool any = !(sum == 0.0f);   // the best entry adds 1, a NaN a NaN
+    const float per_sum = 1.0f / sum, log_sums = MODE == kGradOnly ? 0.0f : logf(st.s) - logf(sum);
     float l = 0.0f;
     for (int j = g.thread; j < a.k; j += threads) {
         float p = 0.0f;
         const int c = e.cls[j];
         if (c >= 0) {
-            const float d = (e.p[j] - top) * inv;
-            p = exp_neg(d) / sum;
+            p = power(e.p[j], top, c2) * per_sum;
             if constexpr (MODE != kGradOnly) {
-                const float logq = Stats::below(Elem<XT>::wide(row.p[c]), st.m) * inv - log_s;
-                if (p != 0.0f) l += p * (d - log_sum - logq);
+                // ln p - ln q
+                const float x = Elem<XT>::wide(row.p[c]) - finite(st.m);
+                if (p != 0.0f) l += p * (((e.p[j] - top) - x) * inv + log_sums);
             }
         }
         e.p[j] = p;
     }
     if constexpr (MODE != kGradOnly) {
         l = g.reduce(l, Sum());
-        *loss = any != 0.0f && !st.empty() ? a.temperature * a.temperature * l : 0.0f;
+        *loss = any && !st.empty() ? a.temperature * a.temperature * l : 0.0f;
     }
     g.sync();                          // the entries are written
-    return any != 0.0f;
+    return any;
 }
 
 // Gradient of the classes of the vectors [lo, hi) of a row.
@@ -154,13 +163,13 @@ __device__ __forceinline__ void gradient(const DistillArgs &a, const Gr &g, int 
                                          bool taught, const Entries &e) {
     using E = Elem<XT>;
     using Raw = typename E::Raw;
-    const float inv = 1.0f / a.temperature;
+    const float c2 = kLog2E / a.temperature;
     Raw *out = static_cast<Raw *>(a.grad) + r * a.ld_grad;
     const bool some = taught && !st.empty();
-    const float base = st.m == -__builtin_inff() ? 0.0f : st.m;
+    const float base = finite(st.m);
     const float gt = a.g[r] * a.temperature;
     const float scale = gt / st.s;
-    auto of = [&](float x) { return some ? exp_neg((x - base) * inv) * scale : 0.0f; };
+    auto of = [&](float x) { return some ? power(x, base, c2) * scale : 0.0f; };
     // 16-byte stores where the gradient's row lies between 16-byte boundaries as the scores' does
     const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
     row.template walk<2>(
@@ -189,7 +198,7 @@ __device__ __forceinline__ void gradient(const DistillArgs &a, const Gr &g, int 
             float p = 0.0f;
             for (int i = 0; i < a.k; ++i)
                 if (e.cls[i] == c) p += e.p[i];
-            const float q = exp_neg((E::wide(row.p[c]) - base) * inv) / st.s;
+            const float q = power(E::wide(row.p[c]), base, c2) / st.s;
             out[c] = E::narrow(gt * (q - p));
         }
 }
@@ -204,7 +213,7 @@ __global__ void __launch_bounds__(Group<G>::kThreads) distill_rows(DistillArgs a
     const int which = G <= 64 ? int(threadIdx.x) / G : 0;
     const Gr g{G <= 64 ? int(threadIdx.x) % G : int(threadIdx.x), box};
     const Entries e{cls[which], p[which]};
-    const float inv = 1.0f / a.temperature;
+    const float c2 = kLog2E / a.temperature;
     for (int64_t r = int64_t(blockIdx.x) * Gr::kInBlock + which; r < a.in.n;
          r += int64_t(gridDim.x) * Gr::kInBlock) {
         const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
@@ -215,9 +224,9 @@ __global__ void __launch_bounds__(Group<G>::kThreads) distill_rows(DistillArgs a
             st.s = v.y;
         } else {
             row.template walk<4>(
-                0, row.vecs, g.thread, G, [&](const u32x4 &v, int) { st.add(row, v, inv); },
-                [&](auto x, int) { st.add(Elem<XT>::wide(x), inv); });
-            st.join(g, inv);
+                0, row.vecs, g.thread, G, [&](const u32x4 &v, int) { st.add(row, v, c2); },
+                [&](auto x, int) { st.add(Elem<XT>::wide(x), c2); });
+            st.join(g, c2);
             if (g.thread == 0) a.stats[r] = float2{st.m, st.s};
         }
         float loss = 0.0f;
@@ -238,7 +247,7 @@ template <dt_dtype XT>
 __global__ void __launch_bounds__(256) distill_part(DistillArgs a) {
     __shared__ float box[4];
     const Group<256> g{int(threadIdx.x), box};
-    const float inv = 1.0f / a.temperature;
+    const float c2 = kLog2E / a.temperature;
     const Row<XT> row(a.in.x, blockIdx.x, a.in.ld, a.in.classes);
     const int per = (row.vecs + a.parts - 1) / a.parts;
     const int lo = int(blockIdx.y) * per < row.vecs ? int(blockIdx.y) * per : row.vecs;
@@ -246,9 +255,9 @@ __global__ void __launch_bounds__(256) distill_part(DistillArgs a) {
     Stats st;
     if (lo < hi)
         row.template walk<4>(
-            lo, hi, g.thread, 256, [&](const u32x4 &v, int) { st.add(row, v, inv); },
-            [&](auto x, int) { st.add(Elem<XT>::wide(x), inv); });
-    st.join(g, inv);
+            lo, hi, g.thread, 256, [&](const u32x4 &v, int) { st.add(row, v, c2); },
+            [&](auto x, int) { st.add(Elem<XT>::wide(x), c2); });
+    st.join(g, c2);
     if (g.thread == 0) a.part[int64_t(blockIdx.x) * a.parts + blockIdx.y] = float2{st.m, st.s};
 }
 
@@ -257,16 +266,16 @@ __global__ void __launch_bounds__(64) distill_join(DistillArgs a) {
     __shared__ int cls[DS_MAX_TOP];
     __shared__ float p[DS_MAX_TOP];
     const Group<64> g{int(threadIdx.x), nullptr};
-    const float inv = 1.0f / a.temperature;
+    const float c2 = kLog2E / a.temperature;
     const int64_t r = blockIdx.x;
     const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
     Stats st;
     for (int i = g.thread; i < a.parts; i += 64) {
         const float2 v = a.part[r * a.parts + i];
-        st.raise(v.x, inv);
-        st.s += v.y * exp_neg(Stats::below(v.x, st.m) * inv);
+        st.raise(v.x, c2);
+        st.s += v.y * power(v.x, finite(st.m), c2);
     }
-    st.join(g, inv);
+    st.join(g, c2);
     if (g.thread == 0) a.stats[r] = float2{st.m, st.s};
     float loss = 0.0f;
     teach<XT, kLossOnly>(a, g, 64, r, row, st, Entries{cls, p}, &loss);
@@ -311,12 +320,9 @@ void run(const DistillArgs &a, hipStream_t stream) {
     } else if (c <= 2048) {
         if (a.g) run_rows<XT, 64, kBoth>(a, stream);
         else run_rows<XT, 64, kLossOnly>(a, stream);
-    } else if (c <= 16384) {
+    } else {
         if (a.g) run_rows<XT, 256, kBoth>(a, stream);
         else run_rows<XT, 256, kLossOnly>(a, stream);
-    } else {
-        if (a.g) run_rows<XT, 1024, kBoth>(a, stream);
-        else run_rows<XT, 1024, kLossOnly>(a, stream);
     }
 }
 

@@ -183,7 +183,7 @@ constexpr int bins_of(int waves) { return waves == 1 ? 256 : 1024; }
 
 template <int WAVES>
 struct Space {
-    Collected c;
+    Collected<WAVES> c;
     uint64_t weight[DS_MAX_TOP];
     uint64_t mass[bins_of(WAVES)];
     uint32_t number[bins_of(WAVES)];
@@ -420,7 +420,7 @@ __device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &
 }
 
 template <dt_dtype XT, int WAVES>
-__global__ void __launch_bounds__(WAVES == 16 ? 1024 : 256) sample_teams(SampleArgs a) {
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) sample_teams(SampleArgs a) {
     constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
     __shared__ Space<WAVES> space[kTeams];
     __shared__ uint64_t box[WAVES];
@@ -436,19 +436,26 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : 256) sample_teams(SampleA
         const Row<XT> row(a.in.x, r, a.in.ld, n);
         const Settings set = settings_of<XT>(a, r);
         const float u = a.u[r];
-        uint32_t mine = 0;
-        row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
-            const uint32_t key = Elem<XT>::key(e);
-            mine = key > mine ? key : mine;
-        });
-        const uint32_t top = t.reduce(mine, Max());
         int label = -1;
-        if (top > 0) {
-            const Weights<XT> weight(set, top, ln);
-            if (set.k <= DS_MAX_TOP && set.k < n) {
-                const int k = best_of_row<XT>(t, row, set.k, mine, top, s.c, [](auto, uint32_t) {});
+        if (set.k <= DS_MAX_TOP && set.k < n) {
+            const int k = best_of_row<XT>(
+                t, row, set.k, s.c, [](const uint32_t *, int) {}, [](const u32x4 &, int) {},
+                [](auto, int) {});
+            if (k > 0) {
+                const Weights<XT> weight(set, comp_key(s.c.best[0]), ln);
                 label = draw_of_few(t, weight, set, k, u, s);
-            } else {
+            }
+        } else {
+            typename Ranks<XT>::Max m;
+            uint32_t single_max = 0;
+            row.template walk<Row<XT>::kAhead>(
+                0, row.vecs, t.thread, t.kThreads,
+                [&](const u32x4 &v4, int) { m.add(Ranks<XT>(v4)); },
+                [&](auto e, int) { single_max = Max()(single_max, Elem<XT>::rank(e)); });
+            const uint32_t top =
+                Elem<XT>::key_of_rank(t.reduce(Max()(single_max, m.rank()), Max()));
+            if (top > 0) {
+                const Weights<XT> weight(set, top, ln);
                 uint64_t cut = 0;
                 if (set.k < n || set.p < 1.0) {
                     const Scale<XT, WAVES> scale(weight);
@@ -488,7 +495,7 @@ template <dt_dtype XT, int WAVES>
 void run_teams(const SampleArgs &a, hipStream_t stream) {
     constexpr int kTeams = WAVES == 1 ? 4 : 1;
     const int64_t blocks = (a.in.n + kTeams - 1) / kTeams;
-    sample_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 16 ? 1024 : 256,
+    sample_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 1 ? 256 : 64 * WAVES,
                               0, stream>>>(a);
 }
 
@@ -506,7 +513,7 @@ void run(const SampleArgs &a, hipStream_t stream) {
     } else if (c <= 8192) {
         run_teams<XT, 4>(a, stream);
     } else {
-        run_teams<XT, 16>(a, stream);
+        run_teams<XT, kBigTeam>(a, stream);
     }
 }
 

@@ -1,10 +1,12 @@
 // The best classes of a row, found by a team of wavefronts.
 //
 // A sort of a whole row would move every element many times; nearly all of them are far from
-// the best k.  Every thread's largest key is known from the first pass over the row.  The k-th
-// largest of these is a bound that k classes of the row reach, and few more do (of 1,024
-// threads' shares and k = 64, about 66): a second pass collects those, and only they are put
-// in order.
+// the best k.  The largest ranks of parts of the row give a bound: where k parts reach it, k
+// classes do, and few more do (of 256 parts and k = 64, about 74).  A walk over the row then
+// collects what reaches the bound, and only that is put in order.  The parts may cover a stretch of the
+// row alone: with k of its parts' maxima above a bound, the whole row has about (row / stretch)
+// times as many classes above it.  So the row is read once from memory, and its first stretch
+// again from the cache.
 #pragma once
 
 #include "scores_common.hpp"
@@ -13,29 +15,13 @@ namespace dscores {
 
 constexpr int kCap = 1024;     // collected classes, in the LDS
 
+template <int WAVES>
 struct Collected {
     uint64_t list[kCap];
     uint64_t best[DS_MAX_TOP];
+    uint32_t maxima[64 * WAVES];
     int count;
 };
-
-// Number of the team's threads that say yes.
-template <int WAVES>
-__device__ __forceinline__ int votes_of(const Team<WAVES> &t, bool yes) {
-    const int c = __popcll(__ballot(yes));
-    if constexpr (WAVES == 1) {
-        return c;
-    } else {
-        int *b = reinterpret_cast<int *>(t.box);
-        t.sync();
-        if (t.lane == 0) b[t.wave] = c;
-        t.sync();
-        int s = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) s += b[w];
-        return s;
-    }
-}
 
 // list[0 .. c) in descending order, in place: a bitonic network over the next power of two,
 // whose places behind c hold 0 (smaller than any class that is collected).
@@ -62,7 +48,7 @@ __device__ __forceinline__ void sort_list(const Team<WAVES> &t, uint64_t *list, 
 // best[0 .. min(k, c)) = the largest of list[0 .. c), in descending order.  Few are ranked by
 // counting the larger ones (every thread reads the whole list, all at the same address).
 template <int WAVES>
-__device__ __forceinline__ void order_best(const Team<WAVES> &t, Collected &s, int c, int k) {
+__device__ __forceinline__ void order_best(const Team<WAVES> &t, Collected<WAVES> &s, int c, int k) {
     if (c <= 256) {
         for (int j = t.thread; j < c; j += t.kThreads) {
             const uint64_t mine = s.list[j];
@@ -109,46 +95,117 @@ __device__ __forceinline__ int count_from(const Team<WAVES> &t, const Row<XT> &r
     return t.reduce(n, Sum());
 }
 
-// s.best[0 .. result) = the row's k best classes, best first (fewer where fewer have a score).
-// mine: the thread's largest key (over its share of the walk `each`), top: the row's (> 0).
-// `also` is called once for each element.
-template <dt_dtype XT, int WAVES, class Also>
-__device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &row, int k, uint32_t mine,
-                           uint32_t top, Collected &s, Also also) {
-    // the bound: lo, where at least k threads' largest keys reach lo (or lo = 1, every score)
-    uint32_t lo = 1, hi = top + 1;      // fewer than k reach hi (unless k = 1)
-    if (k == 1) {
-        lo = top;
-    } else if (votes_of(t, mine > 0) >= k) {
-        // any bound with about k above it will do
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + ((hi - lo) >> 1);
-            const int n = votes_of(t, mine >= mid);
-            if (n < k) {
-                hi = mid;
-            } else {
-                lo = mid;
-                if (n <= k + (k >> 2) + 8) break;
-            }
+// The largest rank that at least k of `parts` (<= 64 * PER) maxima in the LDS reach, or one that few
+// more than k reach; at least `least`.  Every wavefront finds it by itself, with up to PER
+// maxima a lane.
+template <int PER>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, int lane, int k,
+                                             uint32_t least) {
+    uint32_t v[PER];
+    uint32_t lo = least, top = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        v[i] = 64 * i < parts ? maxima[64 * i + lane] : 0u;      // parts is a multiple of 64
+        top = v[i] > top ? v[i] : top;
+    }
+    uint32_t hi = wave_reduce(top, Max()) + 1;                   // none reaches hi
+    auto reach = [&](uint32_t x) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (64 * i < parts) n += __popcll(__ballot(v[i] >= x));
+        return n;
+    };
+    if (hi <= lo || reach(lo) < k) return lo;
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + ((hi - lo) >> 1);
+        const int n = reach(mid);
+        if (n < k) {
+            hi = mid;
+        } else {
+            lo = mid;
+            if (n <= k + (k >> 3) + 4) break;
         }
     }
-    if (t.thread == 0) s.count = 0;
-    t.sync();
-    row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int c) {
-        const uint32_t key = Elem<XT>::key(e);
-        also(e, key);
-        if (key >= lo) {
-            const int at = atomicAdd(&s.count, 1);
-            if (at < kCap) s.list[at] = comp(key, c);
+    return lo;
+}
+
+// s.best[0 .. result) = the row's k best classes, best first (fewer where fewer have a score).
+// While it walks over the row, vector(a, v) is called for its vectors and single(e, c) for the
+// elements before and behind them; `begin` before that, at each attempt, with the largest rank of
+// the stretch.
+template <dt_dtype XT, int WAVES, class FB, class FV, class FE>
+__device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &row, int k,
+                                           Collected<WAVES> &s, FB begin, FV vector, FE single) {
+    using E = Elem<XT>;
+    constexpr int kThreads = Team<WAVES>::kThreads;
+    // so long a stretch that about 200 classes are collected, which are ordered quickly
+    const int64_t want = int64_t(row.vecs) * (k + (k >> 2)) / 200;
+    int stretch = want < row.vecs ? int(want) : row.vecs;
+    stretch = (stretch + kThreads - 1) / kThreads * kThreads;
+    if (stretch > row.vecs) stretch = row.vecs;
+    // parts of the maxima: a thread each, or four threads where those are enough
+    const bool four = kThreads >= 1024 && k <= 64;
+    const int parts = four ? kThreads / 4 : kThreads;
+    int c;
+    for (;;) {
+        typename Ranks<XT>::Max m;
+        uint32_t single_max = 0;
+        row.template walk<Row<XT>::kAhead>(
+            0, stretch, t.thread, kThreads,
+            [&](const u32x4 &a, int) { m.add(Ranks<XT>(a)); },
+            [&](auto e, int) { single_max = Max()(single_max, E::rank(e)); });
+        uint32_t mine = Max()(single_max, m.rank());
+        if (four) {
+            mine = Max()(mine, xor_lane(mine, 1));
+            mine = Max()(mine, xor_lane(mine, 2));
+            if ((t.lane & 3) == 0) s.maxima[t.thread >> 2] = mine;
+        } else {
+            s.maxima[t.thread] = mine;
         }
-    });
-    t.sync();
-    int c = s.count;
-    t.sync();                            // read by all before it is written again
+        if (t.thread == 0) s.count = 0;
+        t.sync();
+        const uint32_t lo = E::from_rank(bound_of<WAVES>(s.maxima, parts, t.lane, k, E::kNone + 1));
+        if (lo == E::kNone + 1 && stretch < row.vecs) {      // a stretch with too few scores
+            stretch = row.vecs;
+            t.sync();
+            continue;
+        }
+        begin(s.maxima, parts);
+        const Filter<XT> filter(lo);
+        auto collect = [&](uint32_t rank, int cls) {
+            const int at = atomicAdd(&s.count, 1);
+            if (at < kCap) s.list[at] = comp(E::key_of_rank(rank), cls);
+        };
+        row.template walk<Row<XT>::kAhead>(
+            0, row.vecs, t.thread, kThreads,
+            [&](const u32x4 &a, int v) {
+                if (filter.any(a)) {
+#pragma unroll
+                    for (int i = 0; i < Row<XT>::kVec; ++i) {
+                        const uint32_t r = E::rank(row.at(a, i));
+                        if (r >= lo) collect(r, row.first(v) + i);
+                    }
+                }
+                vector(a, v);
+            },
+            [&](auto e, int cls) {
+                const uint32_t r = E::rank(e);
+                if (r >= lo) collect(r, cls);
+                single(e, cls);
+            });
+        t.sync();
+        c = s.count;
+        t.sync();                            // read by all before it is written again
+        if (c <= kCap || stretch == row.vecs) break;
+        stretch = row.vecs;
+    }
     if (c > kCap) {
         // Too many equal (or few threads for many classes): the k-th best key itself, by
         // halving, and of the classes that have it the first ones.
-        uint32_t kth = lo, over = top + 1;
+        uint32_t kth = 1, over = 0;
+        for (int i = t.lane; i < parts; i += 64) over = Max()(over, s.maxima[i]);
+        over = E::key_of_rank(wave_reduce(over, Max())) + 1;     // the row's best, and one
         while (over - kth > 1) {
             const uint32_t mid = kth + ((over - kth) >> 1);
             if (count_from(t, row, mid) >= k)

@@ -52,41 +52,90 @@ __global__ void __launch_bounds__(256) top_lanes(TopArgs a) {
         }
 }
 
+// ln 2^y for the sum: e^(x - m) = 2^(x log2 e - m log2 e), whose second product is the same for the
+// whole row.  Its rounding moves the sum's logarithm by at most half a step of m.
+struct Exponent {
+    float base, shift;     // m, -m log2 e
+    __device__ __forceinline__ void set(float m) {
+        base = m;
+        shift = -m * 1.44269504f;
+    }
+    __device__ __forceinline__ float operator()(float x) const {
+        return __builtin_amdgcn_exp2f(fmaf(x, 1.44269504f, shift));
+    }
+};
+
 // A team a row.
 template <dt_dtype XT, int WAVES>
-__global__ void __launch_bounds__(WAVES == 16 ? 1024 : 256) top_teams(TopArgs a) {
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) top_teams(TopArgs a) {
     constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
-    __shared__ Collected space[kTeams];
+    using E = Elem<XT>;
+    __shared__ Collected<WAVES> space[kTeams];
     __shared__ uint64_t box[WAVES];
     const int which = WAVES == 1 ? threadIdx.x >> 6 : 0;
     const int thread = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const Team<WAVES> t{thread, thread & 63, thread >> 6, box};
-    Collected &s = space[which];
+    Collected<WAVES> &s = space[which];
     for (int64_t r = int64_t(blockIdx.x) * kTeams + which; r < a.in.n;
          r += int64_t(gridDim.x) * kTeams) {
         const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
-        uint32_t mine = 0;
-        row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
-            const uint32_t key = Elem<XT>::key(e);
-            mine = key > mine ? key : mine;
-        });
-        const uint32_t top = t.reduce(mine, Max());
-        int found = 0;
+        // the sum is taken relative to the best of the stretch that is looked at first
+        Exponent ex;
         float sum = 0.0f;
-        if (top > 0) {
-            const float m = Elem<XT>::value(top);
-            found = best_of_row<XT>(t, row, a.k, mine, top, s, [&](auto e, uint32_t key) {
+        uint32_t votes = 0;
+        const int found = best_of_row<XT>(
+            t, row, a.k, s,
+            [&](const uint32_t *maxima, int parts) {
+                uint32_t m = 0;
+                for (int i = t.lane; i < parts; i += 64) m = Max()(m, maxima[i]);
+                m = E::key_of_rank(wave_reduce(m, Max()));
+                ex.set(m > 0 ? E::value(m) : 0.0f);
+                sum = 0.0f;
+                votes = 0;
+            },
+            [&](const u32x4 &v4, int) {
+                if constexpr (XT == DT_U8) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) votes = __builtin_amdgcn_sad_u8(v4[i], 0u, votes);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < Row<XT>::kVec; ++i) sum += ex(E::wide(row.at(v4, i)));
+                }
+            },
+            [&](auto x, int) {
                 if constexpr (XT == DT_U8)
-                    sum += float(key);
-                else if (key > 0)
-                    sum += key == top ? 1.0f : exp_neg(Elem<XT>::wide(e) - m);
+                    votes += x;
+                else
+                    sum += ex(E::wide(x));
             });
-            sum = t.reduce(sum, Sum());
+        const uint32_t top = found > 0 ? comp_key(s.best[0]) : 0u;
+        float lse = -__builtin_inff();
+        if (top > 0) {
+            if constexpr (XT == DT_U8) {
+                lse = logf(float(t.reduce(votes, Sum())));
+            } else {
+                const float best = E::value(top);
+                sum = t.reduce(sum, Sum());
+                if (best == __builtin_inff()) {
+                    lse = best;
+                } else if (sum < 1e30f && fabsf(ex.base) <= 1e6f) {
+                    lse = ex.base + logf(sum);
+                } else {
+                    // The best is far above the stretch that the sum is relative to, or so large
+                    // that the rounding of m log2 e is, or there is a NaN: again, term by term.
+                    sum = 0.0f;
+                    row.template each<1>(0, row.vecs, t.thread, t.kThreads, [&](auto x, int) {
+                        const float e = exp_neg(E::wide(x) - best);
+                        sum += e >= 0.0f ? e : 0.0f;
+                    });
+                    lse = best + logf(t.reduce(sum, Sum()));
+                }
+            }
         }
-        if (t.thread == 0) a.lse[r] = log_sum<XT>(top, sum);
+        if (t.thread == 0) a.lse[r] = lse;
         for (int j = t.thread; j < a.k; j += t.kThreads) {
             const uint32_t key = j < found ? comp_key(s.best[j]) : 0u;
-            a.values[r * a.k + j] = key > 0 ? Elem<XT>::value(key) : -__builtin_inff();
+            a.values[r * a.k + j] = key > 0 ? E::value(key) : -__builtin_inff();
             a.index[r * a.k + j] = key > 0 ? comp_class(s.best[j]) : -1;
         }
         t.sync();
@@ -97,7 +146,7 @@ template <dt_dtype XT, int WAVES>
 void run_teams(const TopArgs &a, hipStream_t stream) {
     constexpr int kTeams = WAVES == 1 ? 4 : 1;
     const int64_t blocks = (a.in.n + kTeams - 1) / kTeams;
-    top_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 16 ? 1024 : 256, 0,
+    top_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 1 ? 256 : 64 * WAVES, 0,
                            stream>>>(a);
 }
 
@@ -115,7 +164,7 @@ void run(const TopArgs &a, hipStream_t stream) {
     } else if (c <= 8192 && a.k <= 64) {
         run_teams<XT, 4>(a, stream);
     } else {
-        run_teams<XT, 16>(a, stream);
+        run_teams<XT, kBigTeam>(a, stream);
     }
 }
 

@@ -97,7 +97,7 @@ def _scores_arg(x, votes: bool):
 
 def _vector_arg(v, what: str, shape, dtype, device):
     """A contiguous tensor that the kernels read or write."""
-    if not isinstance(v, torch.Tensor) or v.dtype != dtype or tuple(v.shape) != tuple(shape) or \
+    if not isinstance(v, torch.Tensor) or v.dtype != dtype or v.shape != shape or \
             v.device != device or not v.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s"
                          % (what, dtype, tuple(shape), device))
@@ -110,13 +110,16 @@ class _On:
     The results belong to the stream that the call runs on; inputs that were allocated on another
     stream are kept until this one is through with them."""
 
-    def __init__(self, x, stream, *inputs):
-        if stream is not None and stream.device != x.device:
-            raise ValueError("the stream belongs to %s, the scores to %s" % (stream.device, x.device))
+    __slots__ = ("_guard",)
+
+    def __init__(self, x, stream, inputs):
         self._guard = None
         if stream is not None:
+            if stream.device != x.device:
+                raise ValueError("the stream belongs to %s, the scores to %s"
+                                 % (stream.device, x.device))
             self._guard = torch.cuda.stream(stream)       # sets the stream's device too
-            for t in (x,) + inputs:
+            for t in inputs:
                 if isinstance(t, torch.Tensor):
                     t.record_stream(stream)
         elif _raw_device is None or _raw_device() != x.device.index:
@@ -147,7 +150,7 @@ def top_scores(x, k: int, values=None, index=None, lse=None, stream=None):
                                     ("lse", lse, (n,), torch.float32)):
         if out is not None:
             _vector_arg(out, name, shape, dtype, x.device)
-    with _On(x, stream, values, index, lse) as s:
+    with _On(x, stream, (x, values, index, lse)) as s:
         if values is None:
             values = torch.empty(n, k, dtype=torch.float32, device=x.device)
         if index is None:
@@ -185,7 +188,7 @@ def sample(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, strea
             s.top_k = int(v)
         else:
             setattr(s, name, float(v))
-    with _On(x, stream, u, temperature, top_k, top_p, min_p, out) as raw:
+    with _On(x, stream, (x, u, temperature, top_k, top_p, min_p, out)) as raw:
         if out is None:
             out = torch.empty(n, dtype=torch.int32, device=x.device)
         _check(_lib.ds_sample(ptr, t, n, classes, ld, u.data_ptr(), ctypes.byref(s),
@@ -198,34 +201,36 @@ def _teacher_arg(x, values, index):
     if not isinstance(values, torch.Tensor) or values.dim() != 2 or values.shape[0] != n or \
             not 1 <= values.shape[1] <= MAX_TOP:
         raise ValueError("the teacher's values must be [%d, k] with 1 <= k <= %d" % (n, MAX_TOP))
-    if values.requires_grad:
-        raise ValueError("a teacher takes no gradient: detach its values")
     _vector_arg(values, "values", values.shape, torch.float32, x.device)
     _vector_arg(index, "index", values.shape, torch.int32, x.device)
     return values.shape[1]
 
 
-def _forward(x, values, index, temperature: float, g, grad, stream):
-    ptr, t, n, classes, ld = _scores_arg(x, False)
-    k = _teacher_arg(x, values, index)
-    if g is not None:
-        _vector_arg(g, "grad_loss", (n,), torch.float32, x.device)
-    with _On(x, stream, values, index, g, grad) as s:
-        loss = torch.empty(n, dtype=torch.float32, device=x.device)
-        stats = torch.empty(n, 2, dtype=torch.float32, device=x.device)
-        need = _lib.ds_distill_work_bytes(n, classes)
-        # a workspace of the call's own: calls on several streams, or graphs, never share one
-        work = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-        gp, ld_grad = None, 0
-        if g is not None:
-            if grad is None:
-                grad = torch.empty(n, classes, dtype=x.dtype, device=x.device)
-            gp, _, _, _, ld_grad = _scores_arg(grad, False)
-        _check(_lib.ds_distill(ptr, t, n, classes, ld, values.data_ptr(), index.data_ptr(), k,
-                               float(temperature), None if g is None else g.data_ptr(),
-                               loss.data_ptr(), stats.data_ptr(), gp, ld_grad,
-                               None if work is None else work.data_ptr(), need, s), "ds_distill")
-    return loss, stats, grad
+def _loss(rows, x, values, index, k, temperature, g, grad, ld_grad, s):
+    """ds_distill on stream s, for arguments that are checked: loss and stats."""
+    ptr, t, n, classes, ld = rows
+    loss = torch.empty(n, dtype=torch.float32, device=x.device)
+    stats = torch.empty(n, 2, dtype=torch.float32, device=x.device)
+    need = _lib.ds_distill_work_bytes(n, classes)
+    # a workspace of the call's own: calls on several streams, or graphs, never share one
+    work = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    status = _lib.ds_distill(ptr, t, n, classes, ld, values.data_ptr(), index.data_ptr(), k,
+                             temperature, None if g is None else g.data_ptr(), loss.data_ptr(),
+                             stats.data_ptr(), None if grad is None else grad.data_ptr(), ld_grad,
+                             None if work is None else work.data_ptr(), need, s)
+    if status:
+        _check(status, "ds_distill")
+    return loss, stats
+
+
+def _gradient(rows, values, index, k, temperature, stats, g, grad, ld_grad, s):
+    """ds_distill_backward on stream s, for arguments that are checked."""
+    ptr, t, n, classes, ld = rows
+    status = _lib.ds_distill_backward(ptr, t, n, classes, ld, values.data_ptr(), index.data_ptr(), k,
+                                      temperature, stats.data_ptr(), g.data_ptr(), grad.data_ptr(),
+                                      ld_grad, s)
+    if status:
+        _check(status, "ds_distill_backward")
 
 
 def _grad_out(x, out):
@@ -245,55 +250,61 @@ def distill_grad(x, values, index, grad_loss, temperature: float = 1.0, out=None
     """``ds_distill``: loss (float32 [n]) and gradient of the rows of a student's scores ``x`` in
     one call, for the weights ``grad_loss`` (float32 [n]) that the rows' losses have.  Arguments
     otherwise as ``distill_loss``; ``out`` takes the gradient (x's type and shape)."""
-    _scores_arg(x, False)
+    rows = _scores_arg(x, False)
+    k = _teacher_arg(x, values, index)
+    _vector_arg(grad_loss, "grad_loss", (rows[2],), torch.float32, x.device)
     _grad_out(x, out)
-    if grad_loss is None:
-        raise ValueError("grad_loss must be given")
-    loss, _, grad = _forward(x.detach(), values, index, temperature, grad_loss, out, stream)
-    return loss, grad
+    with _On(x, stream, (x, values, index, grad_loss, out)) as s:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        loss, _ = _loss(rows, x, values, index, k, float(temperature), grad_loss, out,
+                        _scores_arg(out, False)[4], s)
+    return loss, out
 
 
 def distill_forward(x, values, index, temperature: float = 1.0, stream=None):
     """``ds_distill`` without a gradient: (loss, stats); ``distill_backward`` takes the stats."""
-    loss, stats, _ = _forward(x.detach(), values, index, temperature, None, None, stream)
-    return loss, stats
+    rows = _scores_arg(x, False)
+    k = _teacher_arg(x, values, index)
+    with _On(x, stream, (x, values, index)) as s:
+        return _loss(rows, x, values, index, k, float(temperature), None, None, 0, s)
 
 
 def distill_backward(x, values, index, stats, grad_loss, temperature: float = 1.0, out=None,
                      stream=None):
     """``ds_distill_backward``: the gradient, from the stats of ``distill_forward``."""
-    x = x.detach()
-    ptr, t, n, classes, ld = _scores_arg(x, False)
+    rows = _scores_arg(x, False)
     k = _teacher_arg(x, values, index)
-    _vector_arg(stats, "stats", (n, 2), torch.float32, x.device)
-    _vector_arg(grad_loss, "grad_loss", (n,), torch.float32, x.device)
+    _vector_arg(stats, "stats", (rows[2], 2), torch.float32, x.device)
+    _vector_arg(grad_loss, "grad_loss", (rows[2],), torch.float32, x.device)
     _grad_out(x, out)
-    with _On(x, stream, values, index, stats, grad_loss, out) as s:
+    with _On(x, stream, (x, values, index, stats, grad_loss, out)) as s:
         if out is None:
-            out = torch.empty(n, classes, dtype=x.dtype, device=x.device)
-        gp, _, _, _, ld_grad = _scores_arg(out, False)
-        _check(_lib.ds_distill_backward(ptr, t, n, classes, ld, values.data_ptr(),
-                                        index.data_ptr(), k, float(temperature),
-                                        stats.data_ptr(), grad_loss.data_ptr(), gp, ld_grad, s),
-               "ds_distill_backward")
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        _gradient(rows, values, index, k, float(temperature), stats, grad_loss, out,
+                  _scores_arg(out, False)[4], s)
     return out
 
 
 class _Distill(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, values, index, temperature):
-        loss, stats = distill_forward(x, values, index, temperature)
+    def forward(ctx, x, values, index, temperature, rows, k):
+        with _On(x, None, ()) as s:
+            loss, stats = _loss(rows, x, values, index, k, temperature, None, None, 0, s)
         ctx.save_for_backward(x, values, index, stats)
-        ctx.temperature = temperature
+        ctx.more = temperature, rows, k
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         x, values, index, stats = ctx.saved_tensors
-        # g may be a broadcast number (the gradient of a sum)
-        grad = distill_backward(x, values, index, stats, g.contiguous(), ctx.temperature)
-        return grad, None, None, None
+        temperature, rows, k = ctx.more
+        # on the stream of the forward pass; g may be a broadcast number (a sum's gradient)
+        with _On(x, None, ()) as s:
+            grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            _gradient(rows, values, index, k, temperature, stats, g.contiguous(), grad, rows[3], s)
+        return grad, None, None, None, None, None
 
 
 def distill_loss(x, values, index, temperature: float = 1.0):
@@ -304,6 +315,8 @@ def distill_loss(x, values, index, temperature: float = 1.0):
 
     Entries whose index is outside the classes, or whose value is -inf, are left out; a row without
     entries has loss 0.  Differentiable in ``x`` (once); runs on torch's current stream."""
-    _scores_arg(x, False)
-    _teacher_arg(x, values, index)
-    return _Distill.apply(x, values, index, float(temperature))
+    rows = _scores_arg(x, False)
+    k = _teacher_arg(x, values, index)
+    if values.requires_grad:
+        raise ValueError("a teacher takes no gradient: detach its values")
+    return _Distill.apply(x, values, index, float(temperature), rows, k)
