@@ -9,9 +9,15 @@
 
 namespace dscores {
 
-// Rows of few classes are worked on by one lane each, others by teams of 1, 4 or 8 wavefronts.
+// Rows of few classes are worked on by one lane each, others by teams of 1, 4, 8 or 16 wavefronts.
 constexpr int kLaneClasses = 64;
-constexpr int kBigTeam = 8;
+
+// Long rows.  Of teams of 4 wavefronts a compute unit holds four, whose phases overlap (2,048 rows
+// of 131,072 bf16, k = 64: 118 us, with two teams of 8 wavefronts 131 us), but 256 threads find no good
+// bound for many classes.  Where there are no more rows than compute units, a row has one to
+// itself, for 16 wavefronts (one row of 131,072: 15 us, with 8 wavefronts 19 us).
+constexpr int64_t kFewRows = 256;
+constexpr int kQuarter = 96;
 
 struct RowArgs {
     const void *x;

@@ -150,15 +150,33 @@ struct Ranks {
     };
 };
 
-// Whether any element of a vector may reach a bound: of the float types the largest of the widened
-// elements, three operands an instruction, which costs half an operation an element where the
-// ranks cost three.  A NaN may hide the largest or be it: then the answer is yes, and the
-// elements' ranks tell.
+// Whether a vector has elements that reach a bound.  Of the float types the largest of the widened
+// elements is compared, three operands an instruction, which costs half an operation an
+// element where the ranks cost three.  A NaN may hide the largest or be it: then it counts as
+// reaching the bound, and the elements' ranks tell.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
+
+template <dt_dtype XT>
+struct Wide {
+    using E = Elem<XT>;
+    static constexpr int kVec = 16 / E::kBytes, kPerWord = 4 / E::kBytes;
+    float x[kVec];
+    __device__ __forceinline__ explicit Wide(const u32x4 &a) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            x[i] = E::wide(typename E::Raw(a[i / kPerWord] >> (8 * E::kBytes * (i % kPerWord))));
+    }
+    __device__ __forceinline__ float max() const {
+        float m = max3(x[0], x[1], x[2]);
+#pragma unroll
+        for (int i = 3; i + 1 < kVec; i += 2) m = max3(m, x[i], x[i + 1]);
+        return max3(m, x[kVec - 1], x[kVec - 1]);
+    }
+};
 
 template <dt_dtype XT>
 struct Filter {
@@ -168,7 +186,8 @@ struct Filter {
     __device__ __forceinline__ explicit Filter(uint32_t least_rank) : least(least_rank) {
         if constexpr (XT != DT_U8) bound = E::value(E::key_of_rank(least));
     }
-    __device__ __forceinline__ bool any(const u32x4 &a) const {
+    // Whether an element of the vector may reach the bound.
+    __device__ __forceinline__ bool maybe(const u32x4 &a) const {
         if constexpr (XT == DT_U8) {
             // what a number has above least - 1, or nothing
             const u16x2 below = {uint16_t(least - 1), uint16_t(least - 1)};
@@ -181,17 +200,31 @@ struct Filter {
             }
             return some != 0;
         } else {
-            constexpr int kVec = 16 / E::kBytes, kPerWord = 4 / E::kBytes;
-            float x[kVec];
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                x[i] = E::wide(typename E::Raw(a[i / kPerWord] >> (8 * E::kBytes * (i % kPerWord))));
-            float m = max3(x[0], x[1], x[2]);
-#pragma unroll
-            for (int i = 3; i + 1 < kVec; i += 2) m = max3(m, x[i], x[i + 1]);
-            if constexpr (kVec % 2 == 0) m = max3(m, x[kVec - 1], x[kVec - 1]);
-            return !(m < bound);
+            return !(Wide<XT>(a).max() < bound);
         }
+    }
+};
+
+// The largest rank of a part of a row, or, where a NaN hides larger scores from the float types'
+// maximum, a lower one.
+template <dt_dtype XT>
+struct PartMax {
+    using E = Elem<XT>;
+    typename Ranks<XT>::Max ranks;
+    float m = -__builtin_inff();
+    __device__ __forceinline__ void add(const u32x4 &a) {
+        if constexpr (XT == DT_U8) {
+            ranks.add(Ranks<XT>(a));
+        } else {
+            const Wide<XT> w(a);
+            m = max3(m, w.max(), w.x[0]);
+        }
+    }
+    __device__ __forceinline__ uint32_t rank() const {
+        if constexpr (XT == DT_U8)
+            return ranks.rank();
+        else
+            return E::rank(E::narrow(m));                      // exact: it is one of the elements
     }
 };
 
@@ -227,7 +260,10 @@ struct Row {
         return Raw(a[i / kPerWord] >> (8 * E::kBytes * (i % kPerWord)));
     }
     __device__ __forceinline__ u32x4 load_whole(int v) const {
-        return *reinterpret_cast<const u32x4 *>(p + first(v));
+        // a row takes less than 2^32 bytes: an offset of 32 bits to an address that, being the same for
+        // a whole team, stays in scalar registers
+        const char *base = reinterpret_cast<const char *>(p - skew);
+        return *reinterpret_cast<const u32x4 *>(base + (uint32_t(v) << 4));
     }
     // Vector v, whose places outside the row are 0.
     __device__ __forceinline__ u32x4 load(int v) const {
@@ -262,6 +298,34 @@ struct Row {
             for (int u = 0; u < U; ++u) vector(a[u], v + u * threads);
         }
         for (; v < end; v += threads) vector(load_whole(v), v);
+    }
+    // The vectors that lie in the row as a whole: [inner_lo, inner_hi).
+    __device__ __forceinline__ int inner_lo() const { return skew > 0 ? 1 : 0; }
+    __device__ __forceinline__ int inner_hi() const {
+        const int hi = whole(vecs - 1) ? vecs : vecs - 1;
+        return hi > inner_lo() ? hi : inner_lo();
+    }
+    // This thread's share of the vectors [lo, hi), which lie in the row, U loads in flight.
+    template <int U, class FV>
+    __device__ __forceinline__ void inner(int lo, int hi, int thread, int threads, FV vector) const {
+        int v = lo + thread;
+        for (; v + (U - 1) * threads < hi; v += U * threads) {
+            u32x4 a[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) a[u] = load_whole(v + u * threads);
+#pragma unroll
+            for (int u = 0; u < U; ++u) vector(a[u], v + u * threads);
+        }
+        for (; v < hi; v += threads) vector(load_whole(v), v);
+    }
+    // f(element, class) for the elements outside these, one to a thread: fewer than 32, so a team has
+    // a thread for each.
+    template <class F>
+    __device__ __forceinline__ void ends(int thread, F f) const {
+        const int head = inner_lo() == 0 ? 0 : (kVec - skew < n ? kVec - skew : n);
+        const int tail = first(inner_hi()) > head ? first(inner_hi()) : head;
+        const int c = thread < head ? thread : tail + thread - head;
+        if (c < n) f(p[c], c);
     }
     // f(element, class) for all elements of the share.
     template <int U, class F>
@@ -366,6 +430,13 @@ __device__ __forceinline__ T wave_before(T v, int lane, T *all) {
     return s - v;
 }
 
+// Orders a wavefront's accesses of the LDS.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <int WAVES>
 struct Team {
     static constexpr int kThreads = 64 * WAVES;
@@ -374,9 +445,7 @@ struct Team {
 
     __device__ __forceinline__ void sync() const {
         if constexpr (WAVES == 1) {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            wave_fence();
         } else {
             __syncthreads();
         }

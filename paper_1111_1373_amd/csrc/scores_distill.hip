@@ -24,9 +24,7 @@ struct Group {
 
     __device__ __forceinline__ void sync() const {
         if constexpr (G <= 64) {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            wave_fence();
         } else {
             __syncthreads();
         }
@@ -60,7 +58,7 @@ __device__ __forceinline__ float power(float x, float m, float c) {
 }
 __device__ __forceinline__ float finite(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 
-constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kLog2E = 1.44269504f;
 
 // The largest of some scores, and the sum of e^((x - largest) / t) over them.
 struct Stats {
@@ -77,22 +75,16 @@ struct Stats {
         s += power(x, finite(m), c);
     }
     template <dt_dtype XT>
-    __device__ __forceinline__ void add(const Row<XT> &row, const u32x4 &a, float c) {
-        using E = Elem<XT>;
-        constexpr int kVec = Row<XT>::kVec;
-        float x[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = E::wide(row.at(a, i));
+    __device__ __forceinline__ void add(const Row<XT> &, const u32x4 &a, float c) {
         // (a NaN may be the largest here: `raise` passes over it, and the sum keeps it; one that
         // hides a larger score from the maximum has made the sum a NaN as well)
-        float top = max3(x[0], x[1], x[2]);
-#pragma unroll
-        for (int i = 3; i + 1 < kVec; i += 2) top = max3(top, x[i], x[i + 1]);
-        top = max3(top, x[kVec - 1], x[kVec - 1]);
-        raise(top, c);
+        const Wide<XT> w(a);
+        raise(w.max(), c);
         const float base = finite(m);
+        float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) s += power(x[i], base, c);
+        for (int i = 0; i < Row<XT>::kVec; ++i) sum += power(w.x[i], base, c);
+        s += sum;
     }
     template <class Gr>
     __device__ __forceinline__ void join(const Gr &g, float c) {
@@ -156,52 +148,65 @@ __device__ __forceinline__ bool teach(const DistillArgs &a, const Gr &g, int thr
     return any;
 }
 
-// Gradient of the classes of the vectors [lo, hi) of a row.
-template <dt_dtype XT, class Gr>
-__device__ __forceinline__ void gradient(const DistillArgs &a, const Gr &g, int threads, int64_t r,
-                                         const Row<XT> &row, int lo, int hi, const Stats &st,
-                                         bool taught, const Entries &e) {
+// A row's gradient: of all its classes, then again of the teacher's.
+template <dt_dtype XT>
+struct Gradient {
     using E = Elem<XT>;
     using Raw = typename E::Raw;
-    const float c2 = kLog2E / a.temperature;
-    Raw *out = static_cast<Raw *>(a.grad) + r * a.ld_grad;
-    const bool some = taught && !st.empty();
-    const float base = finite(st.m);
-    const float gt = a.g[r] * a.temperature;
-    const float scale = gt / st.s;
-    auto of = [&](float x) { return some ? power(x, base, c2) * scale : 0.0f; };
-    // 16-byte stores where the gradient's row lies between 16-byte boundaries as the scores' does
-    const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
-    row.template walk<2>(
-        lo, hi, g.thread, threads,
-        [&](const u32x4 &v4, int v) {
-            constexpr int kPerWord = 4 / E::kBytes;
-            u32x4 q = {0u, 0u, 0u, 0u};
+    const Row<XT> &row;
+    Raw *out;
+    float c2, base, gt, sum, scale;
+    bool some, same;
+
+    __device__ __forceinline__ Gradient(const DistillArgs &a, int64_t r, const Row<XT> &row_of,
+                                        const Stats &st, bool taught)
+        : row(row_of) {
+        out = static_cast<Raw *>(a.grad) + r * a.ld_grad;
+        c2 = kLog2E / a.temperature;
+        base = finite(st.m);
+        gt = a.g[r] * a.temperature;
+        sum = st.s;
+        scale = gt / st.s;
+        some = taught && !st.empty();
+        // 16-byte stores where its row lies between 16-byte boundaries as the scores' does
+        same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
+    }
+    __device__ __forceinline__ float of(float x) const {
+        return some ? power(x, base, c2) * scale : 0.0f;
+    }
+    // Not kept in the caches, which the next kernel's reads need (see the table of times).
+    __device__ __forceinline__ void vector(const u32x4 &v4, int v) const {
+        constexpr int kPerWord = 4 / E::kBytes;
+        u32x4 q = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int i = 0; i < Row<XT>::kVec; ++i)
-                q[i / kPerWord] |= uint32_t(E::narrow(of(E::wide(row.at(v4, i)))))
-                                   << (8 * E::kBytes * (i % kPerWord));
-            Raw *to = out + row.first(v);
-            if (same) {
-                *reinterpret_cast<u32x4 *>(to) = q;
-            } else {
+        for (int i = 0; i < Row<XT>::kVec; ++i)
+            q[i / kPerWord] |= uint32_t(E::narrow(of(E::wide(row.at(v4, i)))))
+                               << (8 * E::kBytes * (i % kPerWord));
+        Raw *to = out + row.first(v);
+        if (same) {
+            __builtin_nontemporal_store(q, reinterpret_cast<u32x4 *>(to));
+        } else {
 #pragma unroll
-                for (int i = 0; i < Row<XT>::kVec; ++i) to[i] = row.at(q, i);
-            }
-        },
-        [&](Raw x, int c) { out[c] = E::narrow(of(E::wide(x))); });
-    g.sync();                          // a class's first store comes before its second
-    if (some)
-        for (int j = g.thread; j < a.k; j += threads) {
-            const int c = e.cls[j];
-            if (c < row.first(lo) || c >= row.first(hi) || c < 0) continue;
-            float p = 0.0f;
-            for (int i = 0; i < a.k; ++i)
-                if (e.cls[i] == c) p += e.p[i];
-            const float q = power(E::wide(row.p[c]), base, c2) / st.s;
-            out[c] = E::narrow(gt * (q - p));
+            for (int i = 0; i < Row<XT>::kVec; ++i) to[i] = row.at(q, i);
         }
-}
+    }
+    __device__ __forceinline__ void single(Raw x, int c) const { out[c] = E::narrow(of(E::wide(x))); }
+    // The teacher's classes of the vectors [lo, hi), once all of these have their first value.
+    template <class Gr>
+    __device__ __forceinline__ void teacher(const DistillArgs &a, const Gr &g, int threads, int lo,
+                                            int hi, const Entries &e) const {
+        g.sync();
+        if (some)
+            for (int j = g.thread; j < a.k; j += threads) {
+                const int c = e.cls[j];
+                if (c < row.first(lo) || c >= row.first(hi) || c < 0) continue;
+                float p = 0.0f;
+                for (int i = 0; i < a.k; ++i)
+                    if (e.cls[i] == c) p += e.p[i];
+                out[c] = E::narrow(gt * (power(E::wide(row.p[c]), base, c2) / sum - p));
+            }
+    }
+};
 
 template <dt_dtype XT, int G, int MODE>
 __global__ void __launch_bounds__(Group<G>::kThreads) distill_rows(DistillArgs a) {
@@ -236,10 +241,72 @@ __global__ void __launch_bounds__(Group<G>::kThreads) distill_rows(DistillArgs a
             const int per = MODE == kGradOnly ? (row.vecs + a.parts - 1) / a.parts : row.vecs;
             const int lo = MODE == kGradOnly ? int(blockIdx.y) * per : 0;
             const int hi = lo + per < row.vecs ? lo + per : row.vecs;
-            if (lo < hi) gradient<XT>(a, g, G, r, row, lo, hi, st, taught, e);
+            if (lo < hi) {
+                const Gradient<XT> grad(a, r, row, st, taught);
+                row.template walk<2>(
+                    lo, hi, g.thread, G, [&](const u32x4 &v4, int v) { grad.vector(v4, v); },
+                    [&](auto x, int c) { grad.single(x, c); });
+                grad.teacher(a, g, G, lo, hi, e);
+            }
         }
         g.sync();
     }
+}
+
+// Loss and gradient of rows of at most kHeld vectors a thread, which stay in registers between the
+// two: the row crosses the memory once (the second walk of distill_rows finds little of a long
+// row in the caches, which all rows in flight share).
+constexpr int kHeld = 16;
+
+template <dt_dtype XT, int G>
+__global__ void __launch_bounds__(G, 4) distill_held(DistillArgs a) {
+    __shared__ int cls[DS_MAX_TOP];
+    __shared__ float p[DS_MAX_TOP];
+    __shared__ float box[G / 64];
+    const Group<G> g{int(threadIdx.x), box};
+    const Entries e{cls, p};
+    const float c2 = kLog2E / a.temperature;
+    for (int64_t r = blockIdx.x; r < a.in.n; r += gridDim.x) {
+        const Row<XT> row(a.in.x, r, a.in.ld, a.in.classes);
+        u32x4 held[kHeld];
+        Stats st;
+        // the whole vectors' places; opaque at each use, else all are kept in registers
+        const int lo = row.inner_lo(), hi = row.inner_hi();
+        auto place = [&](int i) {
+            int thread = g.thread;
+            asm volatile("" : "+v"(thread));
+            return lo + thread + i * G;
+        };
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int v = place(i);
+            held[i] = row.load_whole(v < hi ? v : lo);       // in any case a place in the row
+        }
+        row.ends(g.thread, [&](auto x, int) { st.add(Elem<XT>::wide(x), c2); });
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            if (place(i) < hi) st.add(row, held[i], c2);
+        }
+        st.join(g, c2);
+        if (g.thread == 0) a.stats[r] = float2{st.m, st.s};
+        float loss = 0.0f;
+        const bool taught = teach<XT, kBoth>(a, g, G, r, row, st, e, &loss);
+        if (g.thread == 0) a.loss[r] = loss;
+        const Gradient<XT> grad(a, r, row, st, taught);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int v = place(i);
+            if (v < hi) grad.vector(held[i], v);
+        }
+        row.ends(g.thread, [&](auto x, int c) { grad.single(x, c); });
+        grad.teacher(a, g, G, 0, row.vecs, e);
+        g.sync();
+    }
+}
+
+template <dt_dtype XT, int G>
+void run_held(const DistillArgs &a, hipStream_t stream) {
+    distill_held<XT, G><<<unsigned(a.in.n < 1048576 ? a.in.n : 1048576), G, 0, stream>>>(a);
 }
 
 // Long rows, few of them: a workgroup for each part of a row, and a wavefront to join them.
@@ -320,9 +387,15 @@ void run(const DistillArgs &a, hipStream_t stream) {
     } else if (c <= 2048) {
         if (a.g) run_rows<XT, 64, kBoth>(a, stream);
         else run_rows<XT, 64, kLossOnly>(a, stream);
+    } else if (!a.g) {
+        run_rows<XT, 256, kLossOnly>(a, stream);
     } else {
-        if (a.g) run_rows<XT, 256, kBoth>(a, stream);
-        else run_rows<XT, 256, kLossOnly>(a, stream);
+        // one vector more than the row's elements need, for the place of its first one
+        const int vecs = (c + Row<XT>::kVec - 1) / Row<XT>::kVec + 1;
+        if (vecs <= 256 * kHeld) run_held<XT, 256>(a, stream);
+        else if (vecs <= 512 * kHeld) run_held<XT, 512>(a, stream);
+        else if (vecs <= 1024 * kHeld) run_held<XT, 1024>(a, stream);
+        else run_rows<XT, 256, kBoth>(a, stream);
     }
 }
 

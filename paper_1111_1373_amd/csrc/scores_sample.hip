@@ -182,12 +182,23 @@ __global__ void __launch_bounds__(256) sample_lanes(SampleArgs a) {
 constexpr int bins_of(int waves) { return waves == 1 ? 256 : 1024; }
 
 template <int WAVES>
-struct Space {
+struct FewSpace {
     Collected<WAVES> c;
     uint64_t weight[DS_MAX_TOP];
+    int label, stay;
+    uint64_t goal;
+};
+
+constexpr int kQueue = 128;      // keys that a wavefront collects before it weighs 64 of them
+
+template <int WAVES>
+struct WideSpace {
     uint64_t mass[bins_of(WAVES)];
     uint32_t number[bins_of(WAVES)];
-    uint64_t part[16];
+    uint64_t list[kCap];
+    uint32_t queue[WAVES][kQueue];
+    uint64_t part[WAVES];
+    int count;
     // answers that one thread finds and all read
     int bin, index;
     uint64_t found, before;
@@ -214,7 +225,7 @@ struct Scale {
 // class that stays, and in s.found the weight of all that stay (if not BY_WEIGHT).
 template <bool BY_WEIGHT, dt_dtype XT, int WAVES>
 __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &row, const Weights<XT> &weight,
-                           const Scale<XT, WAVES> &scale, uint64_t q, Space<WAVES> &s) {
+                           const Scale<XT, WAVES> &scale, uint64_t q, WideSpace<WAVES> &s) {
     constexpr int kBins = bins_of(WAVES), kEach = kBins / Team<WAVES>::kThreads;
     static_assert(kEach >= 1, "");
     // the bin in which it lies
@@ -252,21 +263,23 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
     }
     const uint64_t before_w = s.before;
     const uint64_t rest = BY_WEIGHT ? q - before_w : q - uint64_t(s.index);
-    const int members = int(s.number[bin]);
+    if (t.thread == 0) s.count = 0;
     t.sync();
+    row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int c) {
+        const uint32_t key = Elem<XT>::key(e);
+        if (scale.bin(key) == bin) {
+            const int at = atomicAdd(&s.count, 1);
+            if (at < kCap) s.list[at] = comp(key, c);
+        }
+    });
+    t.sync();
+    const int members = s.count;
     if (members <= kCap) {
-        if (t.thread == 0) s.c.count = 0;
-        t.sync();
-        row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int c) {
-            const uint32_t key = Elem<XT>::key(e);
-            if (scale.bin(key) == bin) s.c.list[atomicAdd(&s.c.count, 1)] = comp(key, c);
-        });
-        t.sync();
-        sort_list(t, s.c.list, members);
+        sort_list(t, s.list, members);
         uint64_t run = 0;
         for (int i0 = 0; i0 < members; i0 += t.kThreads) {
             const int i = i0 + t.thread;
-            const uint64_t wi = i < members ? weight(comp_key(s.c.list[i])) : 0;
+            const uint64_t wi = i < members ? weight(comp_key(s.list[i])) : 0;
             uint64_t all;
             const uint64_t b = run + t.before(wi, &all);
             const bool here = BY_WEIGHT ? (b < rest && rest <= b + wi) : uint64_t(i) + 1 == rest;
@@ -277,7 +290,7 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
             run += all;
         }
         t.sync();
-        return s.c.list[s.index];
+        return s.list[s.index];
     }
     // Too many to collect: the key at which it lies, by halving, and the place among the
     // classes of that key.
@@ -317,7 +330,7 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
 // The drawn class among s.c.best[0 .. k), which are in order.
 template <dt_dtype XT, int WAVES>
 __device__ __forceinline__ int draw_of_few(const Team<WAVES> &t, const Weights<XT> &weight, const Settings &set,
-                           int k, float u, Space<WAVES> &s) {
+                           int k, float u, FewSpace<WAVES> &s) {
     for (int j = t.thread; j < DS_MAX_TOP; j += t.kThreads)
         s.weight[j] = j < k ? weight(comp_key(s.c.best[j])) : 0;
     t.sync();
@@ -345,31 +358,33 @@ __device__ __forceinline__ int draw_of_few(const Team<WAVES> &t, const Weights<X
         stay = wave_reduce(stay, Sum());
         sum = wave_reduce(sum, Sum());
         if (t.lane == 0) {
-            s.index = stay;
-            s.found = target(u, sum);
+            s.stay = stay;
+            s.goal = target(u, sum);
         }
     }
     t.sync();
-    const int stay = s.index;
-    const uint64_t goal = s.found;
+    const int stay = s.stay;
+    const uint64_t goal = s.goal;
     for (int j = t.thread; j < stay; j += t.kThreads) {
         const int c = comp_class(s.c.best[j]);
         uint64_t upto = 0;
 #pragma unroll 8
         for (int i = 0; i < stay; ++i)
             upto += comp_class(s.c.best[i]) <= c ? s.weight[i] : 0;
-        if (upto > goal && upto - s.weight[j] <= goal) s.bin = c;
+        if (upto > goal && upto - s.weight[j] <= goal) s.label = c;
     }
     t.sync();
-    return s.bin;
+    return s.label;
 }
 
 // The drawn class among all that stay: those from `cut` on, of weight `least` or more.
 template <dt_dtype XT, int WAVES>
-__device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &row, const Weights<XT> &weight,
-                           uint64_t cut, uint64_t least, float u, Space<WAVES> &s) {
+__device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &row,
+                                           const Weights<XT> &weight, uint64_t cut, uint64_t least,
+                                           float u, WideSpace<WAVES> &s) {
+    using E = Elem<XT>;
     auto staying = [&](auto e, int c) {
-        const uint32_t key = Elem<XT>::key(e);
+        const uint32_t key = E::key(e);
         if (comp(key, c) < cut) return uint64_t(0);
         const uint64_t w = weight(key);
         return w >= least ? w : uint64_t(0);
@@ -377,26 +392,54 @@ __device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &
     // each wavefront sums a stretch of the row
     const int per = (row.vecs + WAVES - 1) / WAVES;
     auto start = [&](int w) { return w * per < row.vecs ? w * per : row.vecs; };
+    const int from = start(t.wave), to = start(t.wave + 1);
     uint64_t sum = 0;
-    row.template each<1>(start(t.wave), start(t.wave + 1), t.lane, 64,
-                         [&](auto e, int c) { sum += staying(e, c); });
+    if (cut == 0) {
+        row.template each<1>(from, to, t.lane, 64, [&](auto e, int c) { sum += staying(e, c); });
+    } else {
+        // Few stay: their keys are queued, and weighed 64 at a time.
+        uint32_t *queue = s.queue[t.wave];
+        int n = 0;                                           // the same in all lanes
+        auto weigh = [&](uint32_t key) {
+            const uint64_t w = weight(key);
+            sum += w >= least ? w : uint64_t(0);
+        };
+        for (int v0 = from; v0 < to; v0 += 64) {
+            const int v = v0 + t.lane;
+            const u32x4 a = v < to ? row.load(v) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < Row<XT>::kVec; ++i) {
+                const int c = row.first(v) + i;
+                const uint32_t key = E::key(row.at(a, i));
+                const bool yes = v < to && row.has(c) && comp(key, c) >= cut;
+                const uint64_t mask = __ballot(yes);
+                if (mask == 0) continue;
+                if (yes) queue[n + __popcll(mask & ((uint64_t(1) << t.lane) - 1))] = key;
+                n += __popcll(mask);
+                if (n >= 64) {
+                    wave_fence();
+                    weigh(queue[t.lane]);
+                    const uint32_t next = queue[64 + t.lane];
+                    wave_fence();
+                    n -= 64;
+                    if (t.lane < n) queue[t.lane] = next;
+                }
+            }
+        }
+        wave_fence();
+        if (t.lane < n) weigh(queue[t.lane]);
+    }
     sum = wave_reduce(sum, Sum());
     uint64_t all = 0;
-    if constexpr (WAVES == 1) {
-        all = sum;
-    } else {
-        if (t.lane == 0) s.part[t.wave] = sum;
-        t.sync();
+    if (t.lane == 0) s.part[t.wave] = sum;
+    t.sync();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) all += s.part[w];
-    }
+    for (int w = 0; w < WAVES; ++w) all += s.part[w];
     const uint64_t goal = target(u, all);
     // the stretch, then the vector, then the class at which the sum passes the goal
     uint64_t run = 0;
     int which = 0;
-    if constexpr (WAVES > 1) {
-        while (which < WAVES - 1 && run + s.part[which] <= goal) run += s.part[which++];
-    }
+    while (which < WAVES - 1 && run + s.part[which] <= goal) run += s.part[which++];
     const int hi = start(which + 1);
     for (int v0 = start(which); v0 < hi && run <= goal; v0 += t.kThreads) {
         const int v = v0 + t.thread;
@@ -419,72 +462,33 @@ __device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &
     return s.bin;
 }
 
+// Rows of which only few classes stay (FEW: top_k <= 256, or temperature 0), or the others.
+__device__ __forceinline__ bool few_stay(const Settings &s, int n) { return s.k <= DS_MAX_TOP && s.k < n; }
+
 template <dt_dtype XT, int WAVES>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) sample_teams(SampleArgs a) {
-    constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
-    __shared__ Space<WAVES> space[kTeams];
+__global__ void __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES >= 4 ? 4 : 2)
+sample_few(SampleArgs a) {
+    constexpr int kTeams = WAVES == 1 ? 2 : 1;              // of a workgroup
+    __shared__ FewSpace<WAVES> space[kTeams];
     __shared__ uint64_t box[WAVES];
     __shared__ double ln[XT == DT_U8 ? 256 : 1];
     if constexpr (XT == DT_U8) fill_ln(ln);
-    const int which = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const int which = WAVES == 1 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)) : 0;
     const int thread = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const Team<WAVES> t{thread, thread & 63, thread >> 6, box};
-    Space<WAVES> &s = space[which];
+    FewSpace<WAVES> &s = space[which];
     const int n = a.in.classes;
     for (int64_t r = int64_t(blockIdx.x) * kTeams + which; r < a.in.n;
          r += int64_t(gridDim.x) * kTeams) {
-        const Row<XT> row(a.in.x, r, a.in.ld, n);
         const Settings set = settings_of<XT>(a, r);
-        const float u = a.u[r];
+        if (!few_stay(set, n)) continue;
+        const Row<XT> row(a.in.x, r, a.in.ld, n);
         int label = -1;
-        if (set.k <= DS_MAX_TOP && set.k < n) {
-            const int k = best_of_row<XT>(
-                t, row, set.k, s.c, [](const uint32_t *, int) {}, [](const u32x4 &, int) {},
-                [](auto, int) {});
-            if (k > 0) {
-                const Weights<XT> weight(set, comp_key(s.c.best[0]), ln);
-                label = draw_of_few(t, weight, set, k, u, s);
-            }
-        } else {
-            typename Ranks<XT>::Max m;
-            uint32_t single_max = 0;
-            row.template walk<Row<XT>::kAhead>(
-                0, row.vecs, t.thread, t.kThreads,
-                [&](const u32x4 &v4, int) { m.add(Ranks<XT>(v4)); },
-                [&](auto e, int) { single_max = Max()(single_max, Elem<XT>::rank(e)); });
-            const uint32_t top =
-                Elem<XT>::key_of_rank(t.reduce(Max()(single_max, m.rank()), Max()));
-            if (top > 0) {
-                const Weights<XT> weight(set, top, ln);
-                uint64_t cut = 0;
-                if (set.k < n || set.p < 1.0) {
-                    const Scale<XT, WAVES> scale(weight);
-                    constexpr int kBins = bins_of(WAVES);
-                    for (int b = t.thread; b < kBins; b += t.kThreads) {
-                        s.mass[b] = 0;
-                        s.number[b] = 0;
-                    }
-                    t.sync();
-                    row.template each<1>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
-                        const uint32_t key = Elem<XT>::key(e);
-                        const int b = scale.bin(key);
-                        if (b < kBins) {
-                            atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[b]),
-                                      static_cast<unsigned long long>(weight(key)));
-                            atomicAdd(&s.number[b], 1u);
-                        }
-                    });
-                    t.sync();
-                    // by number first: of the rest's weight, top-p's share
-                    cut = end_of<false, XT, WAVES>(
-                        t, row, weight, scale, set.k < n ? uint64_t(set.k) : ~uint64_t(0), s);
-                    const uint64_t all = s.found;
-                    t.sync();
-                    if (set.p < 1.0)
-                        cut = end_of<true, XT, WAVES>(t, row, weight, scale, share(set.p, all), s);
-                }
-                label = draw_of_row(t, row, weight, cut, weight.least(set.min_p), u, s);
-            }
+        const int k = best_of_row<XT>(t, row, set.k, s.c, [](const uint32_t *, int) {},
+                                      [](const u32x4 &) {}, [](auto) {});
+        if (k > 0) {
+            const Weights<XT> weight(set, comp_key(s.c.best[0]), ln);
+            label = draw_of_few(t, weight, set, k, a.u[r], s);
         }
         if (t.thread == 0) a.labels[r] = label;
         t.sync();
@@ -492,11 +496,91 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) sample_teams(Sa
 }
 
 template <dt_dtype XT, int WAVES>
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES >= 4 ? 4 : 2)
+sample_wide(SampleArgs a) {
+    constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
+    __shared__ WideSpace<WAVES> space[kTeams];
+    __shared__ uint64_t box[WAVES];
+    __shared__ double ln[XT == DT_U8 ? 256 : 1];
+    if constexpr (XT == DT_U8) fill_ln(ln);
+    const int which = WAVES == 1 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)) : 0;
+    const int thread = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const Team<WAVES> t{thread, thread & 63, thread >> 6, box};
+    WideSpace<WAVES> &s = space[which];
+    const int n = a.in.classes;
+    for (int64_t r = int64_t(blockIdx.x) * kTeams + which; r < a.in.n;
+         r += int64_t(gridDim.x) * kTeams) {
+        const Settings set = settings_of<XT>(a, r);
+        if (few_stay(set, n)) continue;
+        const Row<XT> row(a.in.x, r, a.in.ld, n);
+        typename Ranks<XT>::Max m;
+        uint32_t single = 0;
+        row.template walk<Row<XT>::kAhead>(
+            0, row.vecs, t.thread, t.kThreads,
+            [&](const u32x4 &v4, int) { m.add(Ranks<XT>(v4)); },
+            [&](auto e, int) { single = Max()(single, Elem<XT>::rank(e)); });
+        const uint32_t top = Elem<XT>::key_of_rank(t.reduce(Max()(single, m.rank()), Max()));
+        int label = -1;
+        if (top > 0) {
+            const Weights<XT> weight(set, top, ln);
+            uint64_t cut = 0;
+            if (set.k < n || set.p < 1.0) {
+                const Scale<XT, WAVES> scale(weight);
+                constexpr int kBins = bins_of(WAVES);
+                for (int b = t.thread; b < kBins; b += t.kThreads) {
+                    s.mass[b] = 0;
+                    s.number[b] = 0;
+                }
+                t.sync();
+                const bool counted = set.k < n;
+                row.template each<2>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
+                    const uint32_t key = Elem<XT>::key(e);
+                    const int b = scale.bin(key);
+                    const uint64_t w = weight(key);
+                    if (b < kBins) {
+                        atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[b]),
+                                  static_cast<unsigned long long>(w));
+                        if (counted) atomicAdd(&s.number[b], 1u);
+                    }
+                });
+                t.sync();
+                // by number first: of the rest's weight, top-p's share
+                cut = end_of<false, XT, WAVES>(
+                    t, row, weight, scale, counted ? uint64_t(set.k) : ~uint64_t(0), s);
+                const uint64_t all = s.found;
+                t.sync();
+                if (set.p < 1.0)
+                    cut = end_of<true, XT, WAVES>(t, row, weight, scale, share(set.p, all), s);
+            }
+            label = draw_of_row(t, row, weight, cut, weight.least(set.min_p), a.u[r], s);
+        }
+        if (t.thread == 0) a.labels[r] = label;
+        t.sync();
+    }
+}
+
+// Settings that only the device sees may ask for either kind of row: then both kernels run, and
+// each passes over the other's rows.
+// A team of 4 wavefronts finds no good bound for many classes, or for a number that only the
+// device knows: one of 8 does.
+template <dt_dtype XT, int WAVES>
 void run_teams(const SampleArgs &a, hipStream_t stream) {
-    constexpr int kTeams = WAVES == 1 ? 4 : 1;
-    const int64_t blocks = (a.in.n + kTeams - 1) / kTeams;
-    sample_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 1 ? 256 : 64 * WAVES,
-                              0, stream>>>(a);
+    constexpr int kFewWaves = WAVES == 4 ? 8 : WAVES;
+    const bool one = !a.set.d_temperature && a.set.temperature == 0.0f;
+    const bool few = one || (!a.set.d_top_k && a.set.top_k >= 1 && a.set.top_k <= DS_MAX_TOP);
+    const bool wide = !few && !a.set.d_top_k && !a.set.d_temperature;
+    auto blocks = [&](int teams) {
+        const int64_t b = (a.in.n + teams - 1) / teams;
+        return unsigned(b < 65536 ? b : 65536);
+    };
+    const bool quarter = one || (!a.set.d_top_k && a.set.top_k <= kQuarter);
+    if (!wide && quarter)
+        sample_few<XT, WAVES><<<blocks(WAVES == 1 ? 2 : 1), WAVES == 1 ? 128 : 64 * WAVES, 0, stream>>>(a);
+    else if (!wide)
+        sample_few<XT, kFewWaves><<<blocks(WAVES == 1 ? 2 : 1), WAVES == 1 ? 128 : 64 * kFewWaves, 0,
+                                   stream>>>(a);
+    if (!few)
+        sample_wide<XT, WAVES><<<blocks(WAVES == 1 ? 4 : 1), WAVES == 1 ? 256 : 64 * WAVES, 0, stream>>>(a);
 }
 
 template <dt_dtype XT>
@@ -510,10 +594,10 @@ void run(const SampleArgs &a, hipStream_t stream) {
         else sample_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
     } else if (c <= kCap) {
         run_teams<XT, 1>(a, stream);       // everything can be collected
-    } else if (c <= 8192) {
+    } else if (c <= 8192 || a.in.n > kFewRows) {
         run_teams<XT, 4>(a, stream);
     } else {
-        run_teams<XT, kBigTeam>(a, stream);
+        run_teams<XT, 16>(a, stream);
     }
 }
 

@@ -14,13 +14,28 @@
 namespace dscores {
 
 constexpr int kCap = 1024;     // collected classes, in the LDS
+constexpr int kSpill = 256;    // queued vectors that a wavefront has no room for
+
+// Vectors of a row's first stretch that are kept in the LDS between the two walks (a compute unit has
+// 160 KiB: one team of 16 wavefronts, two of 8), and vectors that a wavefront can queue.
+template <int WAVES>
+constexpr int kHeldVecs = WAVES == 1 ? 512 : WAVES == 4 ? 1280 : WAVES == 8 ? 3584 : 6144;
+template <int WAVES>
+constexpr int kShare = WAVES == 1 ? 128 : 64;
 
 template <int WAVES>
 struct Collected {
-    uint64_t list[kCap];
+    union {
+        u32x4 held[kHeldVecs<WAVES>];
+        uint64_t list[kCap];   // sorted or ranked, once the walks are over
+    };
     uint64_t best[DS_MAX_TOP];
+    u32x4 queue[WAVES * kShare<WAVES> + kSpill];     // each wavefront's, then the others
+    int place[WAVES * kShare<WAVES> + kSpill];
     uint32_t maxima[64 * WAVES];
-    int count;
+    int counts[WAVES];
+    int spilt, count;
+    uint32_t bound;
 };
 
 // list[0 .. c) in descending order, in place: a bitonic network over the next power of two,
@@ -46,20 +61,34 @@ __device__ __forceinline__ void sort_list(const Team<WAVES> &t, uint64_t *list, 
 }
 
 // best[0 .. min(k, c)) = the largest of list[0 .. c), in descending order.  Few are ranked by
-// counting the larger ones (every thread reads the whole list, all at the same address).
-template <int WAVES>
-__device__ __forceinline__ void order_best(const Team<WAVES> &t, Collected<WAVES> &s, int c, int k) {
-    if (c <= 256) {
-        for (int j = t.thread; j < c; j += t.kThreads) {
-            const uint64_t mine = s.list[j];
-            int rank = 0;
+// counting the larger ones, with as many neighbouring lanes to one entry as the team has.
+template <int LANES, int WAVES>
+__device__ __forceinline__ void rank_list(const Team<WAVES> &t, const uint64_t *list, uint64_t *best,
+                                          int c, int k) {
+    const int part = t.thread & (LANES - 1);
+    for (int j0 = 0; j0 < c; j0 += t.kThreads / LANES) {
+        const int j = j0 + t.thread / LANES;
+        const uint64_t mine = j < c ? list[j] : 0;
+        int rank = 0;
 #pragma unroll 8
-            for (int i = 0; i < c; ++i) rank += s.list[i] > mine;
-            if (rank < k) s.best[rank] = mine;
-        }
+        for (int i = part; i < c; i += LANES) rank += list[i] > mine;
+        rank = wave_reduce<LANES>(rank, Sum());
+        if (part == 0 && j < c && rank < k) best[rank] = mine;
+    }
+}
+
+template <int WAVES>
+__device__ __forceinline__ void order_best(const Team<WAVES> &t, uint64_t *list, uint64_t *best, int c,
+                                           int k) {
+    if (8 * c <= t.kThreads) {
+        rank_list<8>(t, list, best, c, k);
+    } else if (4 * c <= t.kThreads) {
+        rank_list<4>(t, list, best, c, k);
+    } else if (2 * c <= t.kThreads || c <= 128) {
+        rank_list<2>(t, list, best, c, k);
     } else {
-        sort_list(t, s.list, c);
-        for (int j = t.thread; j < k && j < c; j += t.kThreads) s.best[j] = s.list[j];
+        sort_list(t, list, c);
+        for (int j = t.thread; j < k && j < c; j += t.kThreads) best[j] = list[j];
     }
     t.sync();
 }
@@ -96,19 +125,21 @@ __device__ __forceinline__ int count_from(const Team<WAVES> &t, const Row<XT> &r
 }
 
 // The largest rank that at least k of `parts` (<= 64 * PER) maxima in the LDS reach, or one that few
-// more than k reach; at least `least`.  Every wavefront finds it by itself, with up to PER
-// maxima a lane.
+// more than k reach; at least `least`.  For one wavefront, with up to PER maxima a lane.
 template <int PER>
 __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, int lane, int k,
                                              uint32_t least) {
     uint32_t v[PER];
-    uint32_t lo = least, top = 0;
+    uint32_t lo = ~0u, top = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         v[i] = 64 * i < parts ? maxima[64 * i + lane] : 0u;      // parts is a multiple of 64
         top = v[i] > top ? v[i] : top;
+        if (64 * i < parts) lo = v[i] < lo ? v[i] : lo;
     }
     uint32_t hi = wave_reduce(top, Max()) + 1;                   // none reaches hi
+    lo = wave_reduce(lo, Min());                                 // and all reach lo
+    lo = lo > least ? lo : least;
     auto reach = [&](uint32_t x) {
         int n = 0;
 #pragma unroll
@@ -116,7 +147,7 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, 
             if (64 * i < parts) n += __popcll(__ballot(v[i] >= x));
         return n;
     };
-    if (hi <= lo || reach(lo) < k) return lo;
+    if (hi <= lo || reach(lo) < k) return least;
     while (hi - lo > 1) {
         const uint32_t mid = lo + ((hi - lo) >> 1);
         const int n = reach(mid);
@@ -124,88 +155,185 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, 
             hi = mid;
         } else {
             lo = mid;
-            if (n <= k + (k >> 3) + 4) break;
+            if (n <= k + (k >> 3) + 3) break;
         }
     }
     return lo;
 }
 
 // s.best[0 .. result) = the row's k best classes, best first (fewer where fewer have a score).
-// While it walks over the row, vector(a, v) is called for its vectors and single(e, c) for the
-// elements before and behind them; `begin` before that, at each attempt, with the largest rank of
-// the stretch.
+// begin(maxima, parts) is called with the largest ranks of the parts, then vector(a) for the
+// row's whole vectors and single(e) for its other elements; all of it again where the first
+// stretch misleads.
 template <dt_dtype XT, int WAVES, class FB, class FV, class FE>
 __device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &row, int k,
                                            Collected<WAVES> &s, FB begin, FV vector, FE single) {
     using E = Elem<XT>;
-    constexpr int kThreads = Team<WAVES>::kThreads;
-    // so long a stretch that about 200 classes are collected, which are ordered quickly
-    const int64_t want = int64_t(row.vecs) * (k + (k >> 2)) / 200;
-    int stretch = want < row.vecs ? int(want) : row.vecs;
-    stretch = (stretch + kThreads - 1) / kThreads * kThreads;
-    if (stretch > row.vecs) stretch = row.vecs;
-    // parts of the maxima: a thread each, or four threads where those are enough
+    constexpr int kThreads = Team<WAVES>::kThreads, U = 4;
+    const int lo_v = row.inner_lo(), hi_v = row.inner_hi();
+    // Vectors lo_v + [0, held) are kept, a whole number for each thread.  So long a stretch that about
+    // 150 or 230 classes are collected; at least what is kept.
+    int held = kHeldVecs<WAVES> / kThreads * kThreads;
+    if (held > hi_v - lo_v) held = hi_v - lo_v;
+    const int64_t want = int64_t(hi_v - lo_v) * (k + (k >> 2)) / (WAVES == 16 ? 150 : 300);
+    int stretch = lo_v + (want > held ? int(want) : held);
+    if (stretch > hi_v || k > kThreads / 2) stretch = hi_v;
+    // the maxima's parts: a thread each, or four threads where those are enough
     const bool four = kThreads >= 1024 && k <= 64;
     const int parts = four ? kThreads / 4 : kThreads;
-    int c;
+    PartMax<XT> m;
+    row.template inner<U>(lo_v, lo_v + held, t.thread, kThreads, [&](const u32x4 &a, int v) {
+        m.add(a);
+        s.held[v - lo_v] = a;
+    });
+    int seen = lo_v + held;
+    uint32_t end_rank = 0;                  // of the element outside the whole vectors that this
+    int end_class = 0;                      // thread has, if any
+    row.ends(t.thread, [&](auto e, int cls) {
+        end_rank = E::rank(e);
+        end_class = cls;
+    });
+    bool fits;
+    uint32_t lo;
     for (;;) {
-        typename Ranks<XT>::Max m;
-        uint32_t single_max = 0;
-        row.template walk<Row<XT>::kAhead>(
-            0, stretch, t.thread, kThreads,
-            [&](const u32x4 &a, int) { m.add(Ranks<XT>(a)); },
-            [&](auto e, int) { single_max = Max()(single_max, E::rank(e)); });
-        uint32_t mine = Max()(single_max, m.rank());
+        row.template inner<U>(seen, stretch, t.thread, kThreads,
+                              [&](const u32x4 &a, int) { m.add(a); });
+        seen = stretch;
+        uint32_t mine = Max()(end_rank, lo_v < hi_v ? m.rank() : 0u);
         if (four) {
-            mine = Max()(mine, xor_lane(mine, 1));
-            mine = Max()(mine, xor_lane(mine, 2));
+            mine = Max()(mine, partner<1>(mine));
+            mine = Max()(mine, partner<2>(mine));
             if ((t.lane & 3) == 0) s.maxima[t.thread >> 2] = mine;
         } else {
             s.maxima[t.thread] = mine;
         }
-        if (t.thread == 0) s.count = 0;
+        if (t.thread == 0) s.spilt = s.count = 0;
         t.sync();
-        const uint32_t lo = E::from_rank(bound_of<WAVES>(s.maxima, parts, t.lane, k, E::kNone + 1));
-        if (lo == E::kNone + 1 && stretch < row.vecs) {      // a stretch with too few scores
-            stretch = row.vecs;
+        // (one wavefront does: eight that did the same would take the others' instructions)
+        if (t.wave == 0) {
+            lo = four ? bound_of<(WAVES + 3) / 4>(s.maxima, parts, t.lane, k, E::kNone + 1)
+                      : bound_of<WAVES>(s.maxima, parts, t.lane, k, E::kNone + 1);
+            if (t.lane == 0) s.bound = lo;
+        }
+        t.sync();
+        lo = E::from_rank(s.bound);
+        if (lo == E::kNone + 1 && stretch < hi_v) {      // a stretch with too few scores
+            stretch = hi_v;
             t.sync();
             continue;
         }
         begin(s.maxima, parts);
+        row.ends(t.thread, [&](auto e, int) { single(e); });
         const Filter<XT> filter(lo);
-        auto collect = [&](uint32_t rank, int cls) {
+        const int mine_at = t.wave * kShare<WAVES>;
+        int met = 0;                                     // the same in all lanes
+        // Vector v of each lane (lanes behind the row's end: not `in`).  One of which an element
+        // may reach the bound is queued; its elements are looked at later, when every lane has
+        // such a vector.
+        auto visit = [&](const u32x4 &a, int v, bool in) {
+            const bool yes = in && filter.maybe(a);
+            const uint64_t mask = __ballot(yes);
+            if (mask != 0) {
+                int at = met + __popcll(mask & ((uint64_t(1) << t.lane) - 1));
+                met += __popcll(mask);
+                if (yes) {
+                    at = at < kShare<WAVES> ? mine_at + at
+                                            : WAVES * kShare<WAVES> + atomicAdd(&s.spilt, 1);
+                    if (at < WAVES * kShare<WAVES> + kSpill) {
+                        s.queue[at] = a;
+                        s.place[at] = v;
+                    }
+                }
+            }
+            if (in) vector(a);
+        };
+        // Wavefronts walk together; a lane behind the end has the last vector again.  Vectors
+        // that are kept come from the LDS (each thread reads what it wrote).
+        for (int v0 = lo_v + (t.thread & ~63); v0 < hi_v; v0 += U * kThreads) {
+            u32x4 a[U];
+            if (v0 + (U - 1) * kThreads + 63 < lo_v + held) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) a[u] = s.held[v0 - lo_v + u * kThreads + t.lane];
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int v = v0 + u * kThreads + t.lane;
+                    a[u] = row.load_whole(v < hi_v ? v : hi_v - 1);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = v0 + u * kThreads + t.lane;
+                if (v0 + u * kThreads < hi_v) visit(a[u], v, v < hi_v);
+            }
+        }
+        if (t.lane == 0) s.counts[t.wave] = met < kShare<WAVES> ? met : kShare<WAVES>;
+        t.sync();
+        fits = s.spilt <= kSpill;
+        if (fits || stretch == hi_v) break;
+        stretch = hi_v;
+        t.sync();
+    }
+    int c = kCap + 1;
+    uint64_t *list = s.list;
+    if (fits) {
+        auto add = [&](uint32_t rank, int cls) {
             const int at = atomicAdd(&s.count, 1);
             if (at < kCap) s.list[at] = comp(E::key_of_rank(rank), cls);
         };
-        row.template walk<Row<XT>::kAhead>(
-            0, row.vecs, t.thread, kThreads,
-            [&](const u32x4 &a, int v) {
-                if (filter.any(a)) {
+        const int spilt = s.spilt;
+        for (int i = t.thread; i < WAVES * kShare<WAVES> + spilt; i += kThreads) {
+            if (i < WAVES * kShare<WAVES> && i % kShare<WAVES> >= s.counts[i / kShare<WAVES>]) continue;
+            const u32x4 a = s.queue[i];
+            const int cls = row.first(s.place[i]);
 #pragma unroll
-                    for (int i = 0; i < Row<XT>::kVec; ++i) {
-                        const uint32_t r = E::rank(row.at(a, i));
-                        if (r >= lo) collect(r, row.first(v) + i);
-                    }
-                }
-                vector(a, v);
-            },
-            [&](auto e, int cls) {
-                const uint32_t r = E::rank(e);
-                if (r >= lo) collect(r, cls);
-                single(e, cls);
-            });
+            for (int j = 0; j < Row<XT>::kVec; ++j) {
+                const uint32_t r = E::rank(row.at(a, j));
+                if (r >= lo) add(r, cls + j);
+            }
+        }
+        if (end_rank >= lo) add(end_rank, end_class);
         t.sync();
         c = s.count;
         t.sync();                            // read by all before it is written again
-        if (c <= kCap || stretch == row.vecs) break;
-        stretch = row.vecs;
+        if (c > 96 && c <= kCap && k < kThreads) {
+            // Ranking takes the square of their number: those that are surely not among the k
+            // best are left out by a bound on the ones that are there.
+            uint32_t mine = 0;
+            for (int i = t.thread; i < c; i += kThreads) mine = Max()(mine, comp_key(s.list[i]));
+            s.maxima[t.thread] = mine;
+            if (t.thread == 0) s.count = 0;
+            t.sync();
+            if (t.wave == 0) {
+                const uint32_t least = bound_of<WAVES>(s.maxima, kThreads, t.lane, k, 1);
+                if (t.lane == 0) s.bound = least;
+            }
+            t.sync();
+            const uint32_t least = s.bound;
+            uint64_t *fewer = reinterpret_cast<uint64_t *>(s.queue);     // no longer needed
+            constexpr int kRoom = sizeof(s.queue) / sizeof(uint64_t);
+            for (int i = t.thread; i < c; i += kThreads)
+                if (comp_key(s.list[i]) >= least) {
+                    const int at = atomicAdd(&s.count, 1);
+                    if (at < kRoom) fewer[at] = s.list[i];
+                }
+            t.sync();
+            if (s.count <= kRoom) {              // (equal ones may be many)
+                list = fewer;
+                c = s.count;
+            }
+            t.sync();
+        }
     }
     if (c > kCap) {
         // Too many equal (or few threads for many classes): the k-th best key itself, by
         // halving, and of the classes that have it the first ones.
-        uint32_t kth = 1, over = 0;
-        for (int i = t.lane; i < parts; i += 64) over = Max()(over, s.maxima[i]);
-        over = E::key_of_rank(wave_reduce(over, Max())) + 1;     // the row's best, and one
+        const int have = count_from(t, row, 1);
+        k = k < have ? k : have;
+        uint32_t kth = 1, over = 1;
+        row.template each<2>(0, row.vecs, t.thread, t.kThreads,
+                             [&](auto e, int) { over = Max()(over, E::key(e)); });
+        over = t.reduce(over, Max()) + 1;
         while (over - kth > 1) {
             const uint32_t mid = kth + ((over - kth) >> 1);
             if (count_from(t, row, mid) >= k)
@@ -241,7 +369,7 @@ __device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &
         t.sync();
         c = k;
     }
-    order_best(t, s, c, k);
+    order_best(t, list, s.best, c, k);
     return c < k ? c : k;
 }
 

@@ -67,12 +67,12 @@ struct Exponent {
 
 // A team a row.
 template <dt_dtype XT, int WAVES>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) top_teams(TopArgs a) {
-    constexpr int kTeams = WAVES == 1 ? 4 : 1;              // of a workgroup
+__global__ void __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES >= 4 ? 4 : 2) top_teams(TopArgs a) {
+    constexpr int kTeams = WAVES == 1 ? 2 : 1;              // of a workgroup
     using E = Elem<XT>;
     __shared__ Collected<WAVES> space[kTeams];
     __shared__ uint64_t box[WAVES];
-    const int which = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const int which = WAVES == 1 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)) : 0;
     const int thread = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const Team<WAVES> t{thread, thread & 63, thread >> 6, box};
     Collected<WAVES> &s = space[which];
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) top_teams(TopAr
                 sum = 0.0f;
                 votes = 0;
             },
-            [&](const u32x4 &v4, int) {
+            [&](const u32x4 &v4) {
                 if constexpr (XT == DT_U8) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) votes = __builtin_amdgcn_sad_u8(v4[i], 0u, votes);
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) top_teams(TopAr
                     for (int i = 0; i < Row<XT>::kVec; ++i) sum += ex(E::wide(row.at(v4, i)));
                 }
             },
-            [&](auto x, int) {
+            [&](auto x) {
                 if constexpr (XT == DT_U8)
                     votes += x;
                 else
@@ -144,9 +144,9 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) top_teams(TopAr
 
 template <dt_dtype XT, int WAVES>
 void run_teams(const TopArgs &a, hipStream_t stream) {
-    constexpr int kTeams = WAVES == 1 ? 4 : 1;
+    constexpr int kTeams = WAVES == 1 ? 2 : 1;
     const int64_t blocks = (a.in.n + kTeams - 1) / kTeams;
-    top_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 1 ? 256 : 64 * WAVES, 0,
+    top_teams<XT, WAVES><<<unsigned(blocks < 65536 ? blocks : 65536), WAVES == 1 ? 128 : 64 * WAVES, 0,
                            stream>>>(a);
 }
 
@@ -161,10 +161,12 @@ void run(const TopArgs &a, hipStream_t stream) {
         else top_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
     } else if (c <= kCap) {
         run_teams<XT, 1>(a, stream);       // everything can be collected
-    } else if (c <= 8192 && a.k <= 64) {
+    } else if (a.k <= kQuarter && (c <= 8192 || a.in.n > kFewRows)) {
         run_teams<XT, 4>(a, stream);
+    } else if (a.in.n > kFewRows) {
+        run_teams<XT, 8>(a, stream);
     } else {
-        run_teams<XT, kBigTeam>(a, stream);
+        run_teams<XT, 16>(a, stream);
     }
 }
 
