@@ -9,6 +9,8 @@
 #include "scores_lanes.hpp"
 #include "scores_select.hpp"
 
+#include <type_traits>
+
 namespace dscores {
 namespace {
 
@@ -40,52 +42,72 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t row
 }
 
 // e^d for -30 <= d <= 0 as a whole multiple of 2^-42.  e^d = 2^n e^r with n the integer next to
-// d / ln 2 and |r| <= ln 2 / 2; e^r by its Taylor sum up to r^11, whose remainder is below
-// 0.3466^12 / 12! = 6.3e-15, 2^-47.  Adding 2^52 leaves the rounded integer in the low bits.
+// d / ln 2 and |r| <= ln 2 / 2; e^r by the polynomial of degree 9 through its values at the
+// Chebyshev nodes of that range, at most 1.9e-14 off (2^-45).  Adding 2^52 leaves the rounded integer in the low
+// bits.
 __device__ __forceinline__ uint64_t exp_weight(double d) {
     const double n = __builtin_rint(d * 1.4426950408889634);
     const double r = fma(-n, 0.6931471805599453, d);
-    double e = 1.0 / 39916800.0;
-    e = fma(e, r, 1.0 / 3628800.0);
-    e = fma(e, r, 1.0 / 362880.0);
-    e = fma(e, r, 1.0 / 40320.0);
-    e = fma(e, r, 1.0 / 5040.0);
-    e = fma(e, r, 1.0 / 720.0);
-    e = fma(e, r, 1.0 / 120.0);
-    e = fma(e, r, 1.0 / 24.0);
-    e = fma(e, r, 1.0 / 6.0);
-    e = fma(e, r, 0.5);
-    e = fma(e, r, 1.0);
-    e = fma(e, r, 1.0);
+    double e = 2.7632640194122123e-06;
+    e = fma(e, r, 2.488445975018801e-05);
+    e = fma(e, r, 0.00019841190648950985);
+    e = fma(e, r, 0.0013888801749663156);
+    e = fma(e, r, 0.008333333367310203);
+    e = fma(e, r, 0.04166666704055183);
+    e = fma(e, r, 0.1666666666661565);
+    e = fma(e, r, 0.4999999999943859);
+    e = fma(e, r, 1.0000000000000013);
+    e = fma(e, r, 1.0000000000000135);
     const double w = __builtin_amdgcn_ldexp(e, int(n) + 42) + 4503599627370496.0;
     return __builtin_bit_cast(uint64_t, w) & 0xFFFFFFFFFFFFFull;
 }
 
-// Weights of a row's classes by their keys.
+// Weights of a row's classes, by their keys or as they are read (numbers of votes; scores widened to
+// fp32, of which -inf and NaN have weight 0).
 template <dt_dtype XT>
 struct Weights {
+    static constexpr bool kVotes = XT == DT_U8;
+    using Read = typename std::conditional<kVotes, uint32_t, float>::type;
     uint32_t top;        // the best key
-    double m;            // its score
-    double inv;
+    Read best;
+    double m, inv;       // its score, 1 / temperature
     bool counts;
     const double *ln;    // ln of 0 .. 255 (votes)
 
+    static __device__ __forceinline__ Read read(typename Elem<XT>::Raw e) {
+        if constexpr (kVotes)
+            return e;
+        else
+            return Elem<XT>::wide(e);
+    }
     __device__ __forceinline__ Weights(const Settings &s, uint32_t top_key, const double *ln_table)
         : top(top_key), inv(s.inv), counts(s.counts), ln(ln_table) {
-        if constexpr (XT == DT_U8)
+        if constexpr (kVotes) {
+            best = top;
             m = ln[top];
-        else
-            m = double(Elem<XT>::value(top));
+        } else {
+            best = Elem<XT>::value(top);
+            m = double(best);
+        }
     }
     __device__ __forceinline__ double one() const {
         return counts ? double(top) * 17179869184.0 : kOne;          // 2^34 a vote
     }
+    __device__ __forceinline__ uint64_t of(Read x) const {
+        if (kVotes && counts) return uint64_t(x) << 34;
+        double v;
+        if constexpr (kVotes)
+            v = ln[x];
+        else
+            v = double(x);
+        const double d = x == best ? 0.0 : (v - m) * inv;            // of +inf too
+        return d >= -double(kNats) ? exp_weight(d) : 0;
+    }
     __device__ __forceinline__ uint64_t operator()(uint32_t key) const {
-        if (XT == DT_U8 && counts) return uint64_t(key) << 34;
-        const double v = XT == DT_U8 ? ln[key] : double(Elem<XT>::value(key));
-        const double d = (v - m) * inv;
-        if (key == top) return uint64_t(1) << 42;                    // of +inf too
-        return key > 0 && d >= -double(kNats) ? exp_weight(d) : 0;
+        if constexpr (kVotes)
+            return of(key);
+        else
+            return key > 0 ? of(Elem<XT>::value(key)) : 0;
     }
     // the least weight that min_p leaves
     __device__ __forceinline__ uint64_t least(double min_p) const {
@@ -208,15 +230,20 @@ struct WideSpace {
 // lower the bin (each step of the computation keeps the order); kBins for weight 0.
 template <dt_dtype XT, int WAVES>
 struct Scale {
-    uint32_t top;
-    float m, step;
-    __device__ __forceinline__ Scale(const Weights<XT> &w)
-        : top(w.top), m(Elem<XT>::value(w.top)), step(float(w.inv * (bins_of(WAVES) / kNats))) {}
-    __device__ __forceinline__ int bin(uint32_t key) const {
+    using W = Weights<XT>;
+    const W &w;
+    float step;
+    __device__ __forceinline__ explicit Scale(const W &weights)
+        : w(weights), step(float(weights.inv * (bins_of(WAVES) / kNats))) {}
+    __device__ __forceinline__ int bin(typename W::Read x) const {
         constexpr int n = bins_of(WAVES);
-        if (key == top) return 0;
-        const float d = (m - Elem<XT>::value(key)) * step;
-        return key > 0 && d < float(n) ? int(d) : n;
+        float diff;
+        if constexpr (W::kVotes)
+            diff = float(w.m) - float(w.ln[x]);
+        else
+            diff = w.best - x;
+        const float d = x == w.best ? 0.0f : diff * step;
+        return d < float(n) ? int(d) : n;                            // n for a NaN
     }
 };
 
@@ -265,11 +292,10 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
     const uint64_t rest = BY_WEIGHT ? q - before_w : q - uint64_t(s.index);
     if (t.thread == 0) s.count = 0;
     t.sync();
-    row.template each<Row<XT>::kAhead>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int c) {
-        const uint32_t key = Elem<XT>::key(e);
-        if (scale.bin(key) == bin) {
+    row.template each<2>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int c) {
+        if (scale.bin(weight.read(e)) == bin) {
             const int at = atomicAdd(&s.count, 1);
-            if (at < kCap) s.list[at] = comp(key, c);
+            if (at < kCap) s.list[at] = comp(Elem<XT>::key(e), c);
         }
     });
     t.sync();
@@ -299,7 +325,7 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
         int k = 0;
         row.template each<1>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
             const uint32_t key = Elem<XT>::key(e);
-            if (key >= least && scale.bin(key) == bin) {
+            if (key >= least && scale.bin(weight.read(e)) == bin) {
                 sum += weight(key);
                 ++k;
             }
@@ -383,10 +409,18 @@ __device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &
                                            const Weights<XT> &weight, uint64_t cut, uint64_t least,
                                            float u, WideSpace<WAVES> &s) {
     using E = Elem<XT>;
+    // the last class that stays, by its score and its place; none: all stay
+    using Read = typename Weights<XT>::Read;
+    Read last = Read(0);
+    if constexpr (Weights<XT>::kVotes)
+        last = comp_key(cut);
+    else
+        last = cut == 0 ? -__builtin_inff() : E::value(comp_key(cut));
+    const int last_class = cut == 0 ? row.n : comp_class(cut);
+    auto within = [&](Read x, int c) { return x > last || (x == last && c <= last_class); };
     auto staying = [&](auto e, int c) {
-        const uint32_t key = E::key(e);
-        if (comp(key, c) < cut) return uint64_t(0);
-        const uint64_t w = weight(key);
+        const Read x = weight.read(e);
+        const uint64_t w = within(x, c) ? weight.of(x) : uint64_t(0);
         return w >= least ? w : uint64_t(0);
     };
     // each wavefront sums a stretch of the row
@@ -398,28 +432,29 @@ __device__ __forceinline__ int draw_of_row(const Team<WAVES> &t, const Row<XT> &
         row.template each<1>(from, to, t.lane, 64, [&](auto e, int c) { sum += staying(e, c); });
     } else {
         // Few stay: their keys are queued, and weighed 64 at a time.
-        uint32_t *queue = s.queue[t.wave];
+        Read *queue = reinterpret_cast<Read *>(s.queue[t.wave]);
         int n = 0;                                           // the same in all lanes
-        auto weigh = [&](uint32_t key) {
-            const uint64_t w = weight(key);
+        auto weigh = [&](Read x) {
+            const uint64_t w = weight.of(x);
             sum += w >= least ? w : uint64_t(0);
         };
         for (int v0 = from; v0 < to; v0 += 64) {
             const int v = v0 + t.lane;
             const u32x4 a = v < to ? row.load(v) : u32x4{0u, 0u, 0u, 0u};
+            const bool whole = v0 > row.inner_lo() && v0 + 64 <= row.inner_hi();
 #pragma unroll
             for (int i = 0; i < Row<XT>::kVec; ++i) {
                 const int c = row.first(v) + i;
-                const uint32_t key = E::key(row.at(a, i));
-                const bool yes = v < to && row.has(c) && comp(key, c) >= cut;
+                const Read x = weight.read(row.at(a, i));
+                const bool yes = within(x, c) && v < to && (whole || row.has(c));
                 const uint64_t mask = __ballot(yes);
                 if (mask == 0) continue;
-                if (yes) queue[n + __popcll(mask & ((uint64_t(1) << t.lane) - 1))] = key;
+                if (yes) queue[n + __popcll(mask & ((uint64_t(1) << t.lane) - 1))] = x;
                 n += __popcll(mask);
                 if (n >= 64) {
                     wave_fence();
                     weigh(queue[t.lane]);
-                    const uint32_t next = queue[64 + t.lane];
+                    const Read next = queue[64 + t.lane];
                     wave_fence();
                     n -= 64;
                     if (t.lane < n) queue[t.lane] = next;
@@ -533,10 +568,10 @@ sample_wide(SampleArgs a) {
                 }
                 t.sync();
                 const bool counted = set.k < n;
-                row.template each<2>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
-                    const uint32_t key = Elem<XT>::key(e);
-                    const int b = scale.bin(key);
-                    const uint64_t w = weight(key);
+                row.template each<1>(0, row.vecs, t.thread, t.kThreads, [&](auto e, int) {
+                    const auto x = weight.read(e);
+                    const int b = scale.bin(x);
+                    const uint64_t w = weight.of(x);
                     if (b < kBins) {
                         atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[b]),
                                   static_cast<unsigned long long>(w));

@@ -89,8 +89,8 @@ def check_sample(got, x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, note
     """Labels equal to sample()'s, except where a border lies within the weights' rounding.
 
     A weight is rounded to a multiple of 2^-42 of the best one (off by 2^-43) after its 64-bit
-    exponential (2^-47), so sums of up to n weights, and p or u times them, differ from the exact ones by at
-    most 2 n (2^-43 + 2^-47) < n 2^-41 of the best weight.  Where a sum of weights is that near to its
+    exponential (2^-45), so sums of up to n weights, and p or u times them, differ from the exact ones by at
+    most 2 n (2^-43 + 2^-45) < n 2^-41 of the best weight.  Where a sum of weights is that near to its
     border (votes at temperature 1/2 are squares of whole numbers, half of whose sum can be reached
     exactly), both sides of the border are right.  Votes at temperature 1 have no such room."""
     want = sample(x, u, temperature, top_k, top_p, min_p)
