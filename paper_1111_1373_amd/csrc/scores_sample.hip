@@ -137,11 +137,14 @@ __device__ __forceinline__ void fill_ln(double *ln) {
 
 // ---- one lane a row ---------------------------------------------------------------------
 
-template <dt_dtype XT, int CP>
+// COUNTS: votes at temperature 1 in all rows; their numbers are the weights, and sums of 64 of them
+// fit 32 bits (1,000,003 rows of 32 votes by top-p: 44 us with 64-bit weights of either kind).
+template <dt_dtype XT, int CP, bool COUNTS>
 __global__ void __launch_bounds__(256) sample_lanes(SampleArgs a) {
     using O = Order<XT>;
-    __shared__ double ln[XT == DT_U8 ? 256 : 1];
-    if constexpr (XT == DT_U8) fill_ln(ln);
+    using Sum = typename std::conditional<COUNTS, uint32_t, uint64_t>::type;
+    __shared__ double ln[XT == DT_U8 && !COUNTS ? 256 : 1];
+    if constexpr (XT == DT_U8 && !COUNTS) fill_ln(ln);
     const int64_t row = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (row >= a.in.n) return;
     const int n = a.in.classes;
@@ -158,22 +161,30 @@ __global__ void __launch_bounds__(256) sample_lanes(SampleArgs a) {
         a.labels[row] = -1;
         return;
     }
-    const Weights<XT> weight(set, O::key(first), ln);
-    const uint64_t least = weight.least(set.min_p);
+    const Weights<XT> weights(set, O::key(first), ln);
+    auto weight = [&](uint32_t key) -> Sum {
+        if constexpr (COUNTS)
+            return key;
+        else
+            return weights(key);
+    };
+    const Sum least = COUNTS ? Sum(__builtin_ceil(set.min_p * double(O::key(first))))
+                             : Sum(weights.least(set.min_p));
     typename O::T cut = 0;                 // classes from here on stay, in their order
-    uint64_t sum = 0;
+    Sum sum = 0;
     if (set.k < n || set.p < 1.0) {
         sort_registers<CP>(v);
-        uint64_t all = 0;
+        Sum all = 0;
 #pragma unroll
         for (int i = 0; i < CP; ++i)
             if (i < set.k) all += weight(O::key(v[i]));
-        const uint64_t end = share(set.p, all);
-        uint64_t before = 0;
+        const uint64_t most = share(set.p, all);
+        const Sum end = most > uint64_t(Sum(~Sum(0))) ? Sum(~Sum(0)) : Sum(most);
+        Sum before = 0;
 #pragma unroll
         for (int i = 0; i < CP; ++i)
             if (i < set.k && before < end) {
-                const uint64_t w = weight(O::key(v[i]));
+                const Sum w = weight(O::key(v[i]));
                 cut = v[i];
                 before += w;
                 if (w >= least) sum += w;
@@ -183,20 +194,30 @@ __global__ void __launch_bounds__(256) sample_lanes(SampleArgs a) {
     } else {
 #pragma unroll
         for (int i = 0; i < CP; ++i) {
-            const uint64_t w = weight(O::key(v[i]));
+            const Sum w = weight(O::key(v[i]));
             if (w >= least) sum += w;
         }
     }
-    const uint64_t goal = target(a.u[row], sum);
-    uint64_t upto = 0;
+    const Sum goal = Sum(target(a.u[row], sum));
+    Sum upto = 0;
     int label = -1;
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
-        const uint64_t w = weight(O::key(v[i]));
+        const Sum w = weight(O::key(v[i]));
         if (v[i] >= cut && w >= least) upto += w;
         if (label < 0 && upto > goal) label = i;
     }
     a.labels[row] = label;
+}
+
+template <dt_dtype XT, bool COUNTS>
+void run_lanes(const SampleArgs &a, hipStream_t stream) {
+    const unsigned blocks = unsigned((a.in.n + 255) / 256);
+    const int c = a.in.classes;
+    if (c <= 8) sample_lanes<XT, 8, COUNTS><<<blocks, 256, 0, stream>>>(a);
+    else if (c <= 16) sample_lanes<XT, 16, COUNTS><<<blocks, 256, 0, stream>>>(a);
+    else if (c <= 32) sample_lanes<XT, 32, COUNTS><<<blocks, 256, 0, stream>>>(a);
+    else sample_lanes<XT, 64, COUNTS><<<blocks, 256, 0, stream>>>(a);
 }
 
 // ---- a team a row -----------------------------------------------------------------------
@@ -622,11 +643,10 @@ template <dt_dtype XT>
 void run(const SampleArgs &a, hipStream_t stream) {
     const int c = a.in.classes;
     if (c <= kLaneClasses) {
-        const unsigned blocks = unsigned((a.in.n + 255) / 256);
-        if (c <= 8) sample_lanes<XT, 8><<<blocks, 256, 0, stream>>>(a);
-        else if (c <= 16) sample_lanes<XT, 16><<<blocks, 256, 0, stream>>>(a);
-        else if (c <= 32) sample_lanes<XT, 32><<<blocks, 256, 0, stream>>>(a);
-        else sample_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
+        if (XT == DT_U8 && !a.set.d_temperature && a.set.temperature == 1.0f)
+            run_lanes<XT, XT == DT_U8>(a, stream);
+        else
+            run_lanes<XT, false>(a, stream);
     } else if (c <= kCap) {
         run_teams<XT, 1>(a, stream);       // everything can be collected
     } else if (c <= 8192 || a.in.n > kFewRows) {
