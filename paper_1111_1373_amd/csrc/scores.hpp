@@ -18,6 +18,8 @@ constexpr int kLaneClasses = 64;
 // itself, for 16 wavefronts (one row of 131,072: 15 us, with 8 wavefronts 19 us).
 constexpr int64_t kFewRows = 256;
 constexpr int kQuarter = 96;
+// The same for one wavefront, on rows of at most 1,024 classes.
+constexpr int kSixteenth = 32;
 
 struct RowArgs {
     const void *x;

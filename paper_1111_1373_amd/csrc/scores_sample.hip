@@ -621,7 +621,7 @@ sample_wide(SampleArgs a) {
 // device knows: one of 8 does.
 template <dt_dtype XT, int WAVES>
 void run_teams(const SampleArgs &a, hipStream_t stream) {
-    constexpr int kFewWaves = WAVES == 4 ? 8 : WAVES;
+    constexpr int kFewWaves = WAVES == 4 ? 8 : WAVES == 1 ? 4 : WAVES;
     const bool one = !a.set.d_temperature && a.set.temperature == 0.0f;
     const bool few = one || (!a.set.d_top_k && a.set.top_k >= 1 && a.set.top_k <= DS_MAX_TOP);
     const bool wide = !few && !a.set.d_top_k && !a.set.d_temperature;
@@ -629,12 +629,12 @@ void run_teams(const SampleArgs &a, hipStream_t stream) {
         const int64_t b = (a.in.n + teams - 1) / teams;
         return unsigned(b < 65536 ? b : 65536);
     };
-    const bool quarter = one || (!a.set.d_top_k && a.set.top_k <= kQuarter);
+    constexpr int kMost = WAVES == 1 ? kSixteenth : kQuarter;
+    const bool quarter = one || (!a.set.d_top_k && a.set.top_k <= kMost);
     if (!wide && quarter)
         sample_few<XT, WAVES><<<blocks(WAVES == 1 ? 2 : 1), WAVES == 1 ? 128 : 64 * WAVES, 0, stream>>>(a);
     else if (!wide)
-        sample_few<XT, kFewWaves><<<blocks(WAVES == 1 ? 2 : 1), WAVES == 1 ? 128 : 64 * kFewWaves, 0,
-                                   stream>>>(a);
+        sample_few<XT, kFewWaves><<<blocks(1), 64 * kFewWaves, 0, stream>>>(a);
     if (!few)
         sample_wide<XT, WAVES><<<blocks(WAVES == 1 ? 4 : 1), WAVES == 1 ? 256 : 64 * WAVES, 0, stream>>>(a);
 }

@@ -311,7 +311,7 @@ __device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &
             t.sync();
             const uint32_t least = s.bound;
             uint64_t *fewer = reinterpret_cast<uint64_t *>(s.queue);     // no longer needed
-            constexpr int kRoom = sizeof(s.queue) / sizeof(uint64_t);
+            constexpr int kRoom = 2 * (WAVES * kShare<WAVES> + kSpill);      // half a vector each
             for (int i = t.thread; i < c; i += kThreads)
                 if (comp_key(s.list[i]) >= least) {
                     const int at = atomicAdd(&s.count, 1);

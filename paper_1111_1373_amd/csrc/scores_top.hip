@@ -159,9 +159,9 @@ void run(const TopArgs &a, hipStream_t stream) {
         else if (c <= 16) top_lanes<XT, 16><<<blocks, 256, 0, stream>>>(a);
         else if (c <= 32) top_lanes<XT, 32><<<blocks, 256, 0, stream>>>(a);
         else top_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
-    } else if (c <= kCap) {
-        run_teams<XT, 1>(a, stream);       // everything can be collected
-    } else if (a.k <= kQuarter && (c <= 8192 || a.in.n > kFewRows)) {
+    } else if (c <= kCap && a.k <= kSixteenth) {
+        run_teams<XT, 1>(a, stream);
+    } else if (c <= kCap || (a.k <= kQuarter && (c <= 8192 || a.in.n > kFewRows))) {
         run_teams<XT, 4>(a, stream);
     } else if (a.in.n > kFewRows) {
         run_teams<XT, 8>(a, stream);
