@@ -129,6 +129,26 @@ def test_sample(sc, n, classes, kind, how):
         SU.check_sample(got, _host(x), u, **s, note=str(s))
 
 
+@pytest.mark.parametrize("kind", ["f32", "u8"])
+@pytest.mark.parametrize("classes", [5, 64, 65, 100, 255, 256, 257, 1500])
+def test_sample_of_as_many_as_there_are(sc, classes, kind):
+    """top_k at, below and above the number of classes, and around what the kernels split by."""
+    rng = np.random.default_rng(classes)
+    x = _scores(rng, 27, classes, kind)
+    u = rng.random(27).astype(np.float32)
+    ud = torch.from_numpy(u).cuda()
+    for k in (classes - 1, classes, classes + 1, 32, 33, 96, 97, 256, 257):
+        for t in (1.0, 0.0):
+            print("as many", classes, kind, k, t, flush=True)
+            out = torch.full((27,), 123456, dtype=torch.int32, device="cuda")
+            sc.sample(x, ud, t, k, 0.95, out=out)
+            SU.check_sample(_host(out), _host(x), u, t, k, 0.95)
+            per_row = torch.full((27,), k, dtype=torch.int32, device="cuda")
+            out.fill_(123456)
+            sc.sample(x, ud, t, per_row, 0.95, out=out)
+            SU.check_sample(_host(out), _host(x), u, t, k, 0.95)
+
+
 @pytest.mark.parametrize("kind,classes", [("f32", 40), ("bf16", 300), ("f16", 3001), ("u8", 12),
                                           ("bf16", 20_000)])
 def test_sample_settings_of_each_row(sc, kind, classes):
@@ -168,6 +188,30 @@ def test_long_rows_of_few_values(sc, kind, classes, values):
               dict(top_k=classes // 2, top_p=0.7, temperature=0.9)):
         print("few values", kind, classes, values, s, flush=True)
         SU.check_sample(_host(sc.sample(x, ud, **s)), _host(x), u, **s)
+
+
+def test_neighbouring_best_classes(sc):
+    """The best classes side by side, where one wavefront meets most of them, and sorted rows."""
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((8, 60_000)).astype(np.float32)
+    x[0, 4096:4900] += 50
+    x[1, :300] += 50
+    x[2, -700:] += 50
+    x[3] = np.sort(x[3])
+    x[4] = np.sort(x[4])[::-1]
+    x[5] = -INF
+    x[5, 777:900] = rng.standard_normal(123)            # fewer scores than asked for, side by side
+    x[6, ::2] = np.nan
+    x[7, 30_000:] = -INF
+    for rows in (x, np.tile(x, (40, 1))):
+        xd = torch.from_numpy(rows).cuda()
+        for kind in ("f32", "bf16"):
+            xk = xd.to(TYPES[kind])
+            for k in (1, 40, 96, 97, 256):
+                print("neighbours", len(rows), kind, k, flush=True)
+                v, i, _ = sc.top_scores(xk, k)
+                np.testing.assert_array_equal(_host(i)[:8], SU.top_scores(_host(xk)[:8], k)[1])
+                assert torch.equal(i, i[:8].repeat(len(rows) // 8, 1))
 
 
 def _teacher(rng, n, classes, k):
