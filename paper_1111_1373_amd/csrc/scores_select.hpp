@@ -2,11 +2,13 @@
 //
 // A sort of a whole row would move every element many times; nearly all of them are far from
 // the best k.  The largest ranks of parts of the row give a bound: where k parts reach it, k
-// classes do, and few more do (of 256 parts and k = 64, about 74).  A walk over the row then
-// collects what reaches the bound, and only that is put in order.  The parts may cover a stretch of the
-// row alone: with k of its parts' maxima above a bound, the whole row has about (row / stretch)
-// times as many classes above it.  So the row is read once from memory, and its first stretch
-// again from the cache.
+// classes do, and few more do (of 256 parts and k = 64, about 74).  A second walk collects what
+// reaches the bound, and only that is put in order.  The parts may cover a stretch of the row alone:
+// with k of its maxima above a bound, the whole row has about (row / stretch) times as many
+// classes above it.  The stretch stays in the LDS, as far as it fits, so the row is read from memory
+// once.  2,048 rows of 131,072 bf16, k = 64, with their log-sum-exp: 118 us = 4.6 TB/s (a read alone
+// reaches 6.9); of a row's 52 us with three others on its compute unit, 44 are the two walks, bound by
+// loads and by the exponentials' instructions, and 6 finding the bounds and collecting.
 #pragma once
 
 #include "scores_common.hpp"
