@@ -12,14 +12,17 @@ namespace dscores {
 // Rows of few classes are worked on by one lane each, others by teams of 1, 4, 8 or 16 wavefronts.
 constexpr int kLaneClasses = 64;
 
-// Long rows.  Of teams of 4 wavefronts a compute unit holds four, whose phases overlap (2,048 rows
-// of 131,072 bf16, k = 64: 118 us, with two teams of 8 wavefronts 131 us), but 256 threads find no good
-// bound for many classes.  Where there are no more rows than compute units, a row has one to
-// itself, for 16 wavefronts (one row of 131,072: 15 us, with 8 wavefronts 19 us).
-constexpr int64_t kFewRows = 256;
+// Long rows (times of top_scores on rows of 131,072 bf16, k = 64).  Where there are no more rows
+// than compute units, each has one to itself, for 16 wavefronts (1 row: 20 us, 28 with 8; 256
+// rows: 25 and 35).  Of teams of 4 wavefronts a compute unit holds four, whose phases overlap: they pay from
+// as many rows on (2,048 rows: 126 us, 142 with 8 wavefronts; 257 rows: 35 and 29).
+constexpr int64_t kFewRows = 256, kManyRows = 1024;
+// 256 threads find no good bound for many classes (2,048 rows, k = 96: 132 us, 138 with 8
+// wavefronts; k = 128: 154 and 150).
 constexpr int kQuarter = 96;
-// The same for one wavefront, on rows of at most 1,024 classes.
-constexpr int kSixteenth = 32;
+// The same for one wavefront, on rows of at most 1,024 classes (60,000 rows of 1,000 bf16, k = 48:
+// 305 us, 429 with 4 wavefronts; k = 60: 502 and 476; fp32, k = 200: 1,725 and 953).
+constexpr int kSixteenth = 48;
 
 struct RowArgs {
     const void *x;

@@ -161,7 +161,7 @@ void run(const TopArgs &a, hipStream_t stream) {
         else top_lanes<XT, 64><<<blocks, 256, 0, stream>>>(a);
     } else if (c <= kCap && a.k <= kSixteenth) {
         run_teams<XT, 1>(a, stream);
-    } else if (c <= kCap || (a.k <= kQuarter && (c <= 8192 || a.in.n > kFewRows))) {
+    } else if (c <= kCap || (a.k <= kQuarter && (c <= 8192 || a.in.n >= kManyRows))) {
         run_teams<XT, 4>(a, stream);
     } else if (a.in.n > kFewRows) {
         run_teams<XT, 8>(a, stream);
