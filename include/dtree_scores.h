@@ -86,7 +86,7 @@ typedef struct {
  *             and above as the largest number below 1)
  *   d_labels  n int32: the class; -1 for an empty row
  * Weights are computed in 64 bits and added as whole multiples of 2^-42 of the best class's,
- * so the result does not depend on any order of summation; a class more than 29 nats (times
+ * so the result does not depend on any order of summation; a class more than 30 nats (times
  * the temperature) below the best is never drawn.  Of scores of +inf, all have weight 1 and
  * no finite score has any.  Votes at temperature 1 have their exact number as weight.
  * Errors: as ds_top_scores; DT_ERR_INVALID_ARG also for settings out of range.
