@@ -25,6 +25,16 @@ constexpr int kHeldVecs = WAVES == 1 ? 512 : WAVES == 4 ? 1280 : WAVES == 8 ? 35
 template <int WAVES>
 constexpr int kShare = WAVES == 1 ? 128 : 64;
 
+// Entries of the list that fewer candidates go to, in the place of the queue, half a vector each:
+// sort_list takes the next power of two, and a list has at most kCap.
+constexpr int power_of_two_below(int n) {
+    int p = 64;
+    while (2 * p <= n && 2 * p <= kCap) p *= 2;
+    return p;
+}
+template <int WAVES>
+constexpr int kFewerRoom = power_of_two_below(2 * (WAVES * kShare<WAVES> + kSpill));
+
 template <int WAVES>
 struct Collected {
     union {
@@ -40,8 +50,9 @@ struct Collected {
     uint32_t bound;
 };
 
-// list[0 .. c) in descending order, in place: a bitonic network over the next power of two,
-// whose places behind c hold 0 (smaller than any class that is collected).
+// list[0 .. c) in descending order, in place: a bitonic network over the next power of two (at
+// least 64), for which the list has room, and whose places behind c hold 0 (smaller than any class that is
+// collected).
 template <int WAVES>
 __device__ __forceinline__ void sort_list(const Team<WAVES> &t, uint64_t *list, int c) {
     int n = 64;
@@ -313,7 +324,8 @@ __device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &
             t.sync();
             const uint32_t least = s.bound;
             uint64_t *fewer = reinterpret_cast<uint64_t *>(s.queue);     // no longer needed
-            constexpr int kRoom = 2 * (WAVES * kShare<WAVES> + kSpill);      // half a vector each
+            constexpr int kRoom = kFewerRoom<WAVES>;
+            static_assert(sizeof(s.queue) >= sizeof(uint64_t) * kRoom && (kRoom & (kRoom - 1)) == 0, "");
             for (int i = t.thread; i < c; i += kThreads)
                 if (comp_key(s.list[i]) >= least) {
                     const int at = atomicAdd(&s.count, 1);

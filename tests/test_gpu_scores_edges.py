@@ -1,0 +1,86 @@
+"""Operators on rows of class scores where their kernels change what they do: many equal scores, the
+ends of the types' ranges, and shapes that only one variant works on.  Plain implementations in 64
+bits and the derivation of the tolerances: scoreutil.py, test_gpu_scores.py."""
+import numpy as np
+import pytest
+
+from tests import scoreutil as SU
+from tests.test_gpu_scores import EPS, INF, TYPES, _host
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def sc():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1111_1373_amd import scores
+    return scores
+
+
+def _check_top(sc, x, want_of, k, note):
+    """top_scores of x, whose rows repeat the rows of want_of."""
+    print("top", note, tuple(x.shape), k, flush=True)
+    values, index, lse = (_host(v) for v in sc.top_scores(x, k))
+    want_v, want_i, want_l = SU.top_scores(want_of, k)
+    at = np.arange(len(x)) % len(want_of)
+    np.testing.assert_array_equal(index, want_i[at])
+    if x.dtype == torch.uint8:
+        np.testing.assert_allclose(values, want_v[at], rtol=4 * EPS)
+    else:
+        np.testing.assert_array_equal(values, want_v[at].astype(np.float32))
+    got, want = lse.astype(np.float64), want_l[at]
+    ok = np.isfinite(want)
+    np.testing.assert_array_equal(got[~ok], want[~ok])
+    err = np.abs(got[ok] - want[ok])
+    tol = (x.shape[1] / 64 + 16) * EPS + 2 * EPS * np.abs(want[ok])
+    assert (err <= tol).all(), err.max()
+
+
+def _tied_rows(rng, classes, kind):
+    """Rows of more equal best scores than a wavefront's short list takes, beside others."""
+    rows = np.stack([rng.permutation(classes) % 40 + 1 for _ in range(8)]).astype(np.float32)
+    rows[0] = 7                                                 # one value
+    rows[2, :] = 3                                              # a few better ones before the ties
+    rows[2, rng.integers(0, classes, 5)] = [41, 43, 47, 53, 59]
+    rows[4] = 9                                                 # just over 512 ties
+    rows[4, rng.permutation(classes)[513:]] = 2
+    rows[5, : classes // 2] = 60
+    rows[6] = 5
+    rows[6, -3:] = 6
+    if kind != "u8":
+        rows -= 30
+    return torch.from_numpy(rows).to(TYPES[kind])
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "u8"])
+@pytest.mark.parametrize("classes", [513, 600, 700, 768, 769, 1000, 1024])
+def test_many_equal_scores_in_short_rows(sc, classes, kind):
+    rng = np.random.default_rng([classes, len(kind)])
+    rows = _tied_rows(rng, classes, kind)
+    x = rows.cuda()
+    for k in (1, 8, 47, 48, 49):
+        _check_top(sc, x, _host(rows), k, "ties " + kind)
+        u = rng.random(len(rows)).astype(np.float32)
+        for s in (dict(top_k=k), dict(top_k=k, top_p=0.6, temperature=1.5)):
+            print("sample", s, flush=True)
+            got = _host(sc.sample(x, torch.from_numpy(u).cuda(), **s))
+            SU.check_sample(got, _host(rows), u, **s)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "u8"])
+def test_many_equal_scores_in_many_rows(sc, kind):
+    """More rows than wavefronts that are launched, so each takes a second one."""
+    rng = np.random.default_rng(len(kind))
+    rows = _tied_rows(rng, 600, kind)
+    n = 2 * 65536 + 1003
+    x = rows.cuda().repeat(n // len(rows) + 1, 1)[:n].contiguous()
+    for k in (3, 48):
+        _check_top(sc, x, _host(rows), k, "many rows " + kind)
+    u = rng.random(len(rows)).astype(np.float32)
+    ud = torch.from_numpy(u).cuda().repeat(n // len(rows) + 1)[:n].contiguous()
+    got = _host(sc.sample(x, ud, 1.0, 20, 0.7))
+    SU.check_sample(got[: len(rows)], _host(rows), u, 1.0, 20, 0.7)
+    np.testing.assert_array_equal(got, got[np.arange(n) % len(rows)])
