@@ -292,18 +292,25 @@ class _Distill(torch.autograd.Function):
         with _On(x, None, ()) as s:
             loss, stats = _loss(rows, x, values, index, k, temperature, None, None, 0, s)
         ctx.save_for_backward(x, values, index, stats)
-        ctx.more = temperature, rows, k
+        ctx.temperature = temperature
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
+        # Saved tensors need not come back where, or with the strides that, they were saved (hooks,
+        # checkpointing): everything is taken from those that did.
         x, values, index, stats = ctx.saved_tensors
-        temperature, rows, k = ctx.more
         # on the stream of the forward pass; g may be a broadcast number (a sum's gradient)
         with _On(x, None, ()) as s:
+            if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+                x = x.contiguous()
+            rows = _scores_arg(x, False)
+            values, index, stats = values.contiguous(), index.contiguous(), stats.contiguous()
+            k = _teacher_arg(x, values, index)
+            _vector_arg(stats, "stats", (rows[2], 2), torch.float32, x.device)
             grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            _gradient(rows, values, index, k, temperature, stats, g.contiguous(), grad, rows[3], s)
+            _gradient(rows, values, index, k, ctx.temperature, stats, g.contiguous(), grad, rows[3], s)
         return grad, None, None, None, None, None
 
 

@@ -84,3 +84,53 @@ def test_many_equal_scores_in_many_rows(sc, kind):
     got = _host(sc.sample(x, ud, 1.0, 20, 0.7))
     SU.check_sample(got[: len(rows)], _host(rows), u, 1.0, 20, 0.7)
     np.testing.assert_array_equal(got, got[np.arange(n) % len(rows)])
+
+
+def _student(rng, n, classes, k, kind, how):
+    """Scores (a leaf, and the rows of it that are used) and a teacher."""
+    wide = torch.from_numpy(rng.standard_normal((n, classes + 8)).astype(np.float32)).to(TYPES[kind])
+    leaf = wide.cuda().requires_grad_()
+    values = torch.from_numpy(rng.standard_normal((n, k)).astype(np.float32)).cuda()
+    index = torch.from_numpy(rng.integers(0, classes, (n, k)).astype(np.int32)).cuda()
+    return leaf, (lambda t: t[:, 3:3 + classes]) if how == "strided" else (lambda t: t[:, :classes] * 1), \
+        values, index
+
+
+@pytest.mark.parametrize("kind,classes", [("f32", 40), ("bf16", 700), ("f16", 20_001)])
+@pytest.mark.parametrize("how", ["dense", "strided"])
+def test_gradient_through_saved_tensors(sc, kind, classes, how):
+    """Hooks, host memory and checkpointing give the gradient that the plain backward pass gives,
+    with the first scores' memory overwritten before it."""
+    from torch.utils.checkpoint import checkpoint
+    rng = np.random.default_rng(classes)
+    leaf, rows_of, values, index = _student(rng, 24, classes, 6, kind, how)
+    g = torch.from_numpy(rng.random(24).astype(np.float32)).cuda()
+
+    def gradient(contextual):
+        def head(t):
+            return sc.distill_loss(rows_of(t * 1), values, index, 2.0)
+        loss = contextual(head)
+        spoil = [torch.full_like(leaf, 99.0) for _ in range(4)]      # what was freed is taken again
+        grad, = torch.autograd.grad(loss, leaf, g)
+        del spoil
+        return grad
+
+    def with_hooks(pack, unpack):
+        def run(head):
+            with torch.autograd.graph.saved_tensors_hooks(pack, unpack):
+                return head(leaf)
+        return run
+
+    def on_cpu(head):
+        with torch.autograd.graph.save_on_cpu():
+            return head(leaf)
+
+    print("saved tensors", kind, classes, how, flush=True)
+    want = gradient(lambda head: head(leaf))
+    assert (want != 0).any()
+    for contextual in (with_hooks(lambda t: t.clone(), lambda t: t),
+                       with_hooks(lambda t: t, lambda t: t.clone()),
+                       with_hooks(lambda t: t.clone(),
+                                  lambda t: t.t().contiguous().t() if t.dim() == 2 else t),
+                       on_cpu, lambda head: checkpoint(head, leaf, use_reentrant=False)):
+        np.testing.assert_array_equal(_host(gradient(contextual)), _host(want))
