@@ -354,7 +354,8 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
         *count = t.reduce(k, Sum());
         return t.reduce(sum, Sum());
     };
-    uint32_t lo = 1, hi = weight.top + 1;      // from(lo) >= rest > from(hi)
+    // from(lo) >= rest > from(hi), modulo 2^32: the largest key of fp32, +inf, is 2^32 - 1
+    uint32_t lo = 1, hi = weight.top + 1;
     int count;
     while (hi - lo > 1) {
         const uint32_t mid = lo + ((hi - lo) >> 1);
@@ -364,7 +365,7 @@ __device__ __forceinline__ uint64_t end_of(const Team<WAVES> &t, const Row<XT> &
         else
             hi = mid;
     }
-    const uint64_t above = hi > weight.top ? (count = 0, uint64_t(0)) : from(hi, &count);
+    const uint64_t above = hi - 1 == weight.top ? (count = 0, uint64_t(0)) : from(hi, &count);
     const uint64_t one = weight(lo);
     const uint64_t nth = BY_WEIGHT ? (rest - above + one - 1) / one : rest - uint64_t(count);
     const int c = nth_equal<XT>(t, row, lo, int(nth), &s.index);

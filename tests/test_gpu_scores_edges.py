@@ -134,3 +134,24 @@ def test_gradient_through_saved_tensors(sc, kind, classes, how):
                                   lambda t: t.t().contiguous().t() if t.dim() == 2 else t),
                        on_cpu, lambda head: checkpoint(head, leaf, use_reentrant=False)):
         np.testing.assert_array_equal(_host(gradient(contextual)), _host(want))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("classes", [5_000, 40_000])
+def test_many_infinite_scores(sc, kind, classes):
+    """More classes of +inf than a team collects: all have the same weight, the others none."""
+    rng = np.random.default_rng([classes, len(kind)])
+    x = rng.standard_normal((6, classes)).astype(np.float32)
+    for r, many in enumerate((1, 1024, 1025, 1500, 4000, classes)):
+        x[r, rng.permutation(classes)[:many]] = INF
+    x = torch.from_numpy(x).to(TYPES[kind])
+    xd = x.cuda()
+    for k in (1, 50, 200):
+        _check_top(sc, xd, _host(x), k, "infinite " + kind)
+    for _ in range(3):
+        u = rng.random(6).astype(np.float32)
+        ud = torch.from_numpy(u).cuda()
+        for s in (dict(top_p=0.3), dict(top_p=0.9), dict(top_k=700), dict(top_k=1400, top_p=0.5),
+                  dict(top_k=200), dict(top_p=0.9, temperature=0.3), dict(min_p=0.5)):
+            print("sample, infinite", kind, classes, s, flush=True)
+            SU.check_sample(_host(sc.sample(xd, ud, **s)), _host(x), u, **s, note=str(s))
