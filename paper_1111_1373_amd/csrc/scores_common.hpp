@@ -152,8 +152,13 @@ struct Ranks {
 
 // Whether a vector has elements that reach a bound.  Of the float types the largest of the widened
 // elements is compared, three operands an instruction, which costs half an operation an
-// element where the ranks cost three.  A NaN may hide the largest or be it: then it counts as
-// reaching the bound, and the elements' ranks tell.
+// element where the ranks cost three.  A NaN is passed over, unless there is nothing else: then it counts
+// as reaching the bound, and the elements' ranks tell.  A signalling NaN is passed over as well once
+// quiet_max() was called; in the IEEE mode in which kernels start it makes max3 lose what came before it.
+__device__ __forceinline__ void quiet_max() {
+    constexpr int kMode = 1, kIeee = 9;                // hardware register, bit of it
+    __builtin_amdgcn_s_setreg(kMode | kIeee << 6 | (1 - 1) << 11, 0);
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -205,8 +210,7 @@ struct Filter {
     }
 };
 
-// The largest rank of a part of a row, or, where a NaN hides larger scores from the float types'
-// maximum, a lower one.
+// The largest rank of a part of a row (quiet_max() before it, as for Filter).
 template <dt_dtype XT>
 struct PartMax {
     using E = Elem<XT>;

@@ -525,6 +525,7 @@ __device__ __forceinline__ bool few_stay(const Settings &s, int n) { return s.k 
 template <dt_dtype XT, int WAVES>
 __global__ void __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES >= 4 ? 4 : 2)
 sample_few(SampleArgs a) {
+    if constexpr (XT != DT_U8) quiet_max();
     constexpr int kTeams = WAVES == 1 ? 2 : 1;              // of a workgroup
     __shared__ FewSpace<WAVES> space[kTeams];
     __shared__ uint64_t box[WAVES];

@@ -177,7 +177,7 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, 
 // s.best[0 .. result) = the row's k best classes, best first (fewer where fewer have a score).
 // begin(maxima, parts) is called with the largest ranks of the parts, then vector(a) for the
 // row's whole vectors and single(e) for its other elements; all of it again where the first
-// stretch misleads.
+// stretch misleads.  Kernels call quiet_max() before.
 template <dt_dtype XT, int WAVES, class FB, class FV, class FE>
 __device__ __forceinline__ int best_of_row(const Team<WAVES> &t, const Row<XT> &row, int k,
                                            Collected<WAVES> &s, FB begin, FV vector, FE single) {

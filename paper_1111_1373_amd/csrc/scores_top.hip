@@ -68,6 +68,7 @@ struct Exponent {
 // A team a row.
 template <dt_dtype XT, int WAVES>
 __global__ void __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES >= 4 ? 4 : 2) top_teams(TopArgs a) {
+    if constexpr (XT != DT_U8) quiet_max();
     constexpr int kTeams = WAVES == 1 ? 2 : 1;              // of a workgroup
     using E = Elem<XT>;
     __shared__ Collected<WAVES> space[kTeams];

@@ -155,3 +155,39 @@ def test_many_infinite_scores(sc, kind, classes):
                   dict(top_k=200), dict(top_p=0.9, temperature=0.3), dict(min_p=0.5)):
             print("sample, infinite", kind, classes, s, flush=True)
             SU.check_sample(_host(sc.sample(xd, ud, **s)), _host(x), u, **s, note=str(s))
+
+
+# signalling and quiet, of both signs
+NANS = {"f32": (torch.int32, (0x7FA00000, 0x7F800001, 0x7FC00000, 0xFFA00000 - (1 << 32), -1)),
+        "f16": (torch.int16, (0x7D00, 0x7C01, 0x7E00, 0xFD00 - (1 << 16), -1)),
+        "bf16": (torch.int16, (0x7FA0, 0x7F81, 0x7FC0, 0xFFA0 - (1 << 16), -1))}
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,classes", [(40, 50), (40, 300), (16, 1024), (16, 5_000), (6, 40_001),
+                                       (300, 9_000), (1100, 8_200)])
+def test_every_kind_of_nan(sc, n, classes, kind):
+    """A NaN, signalling ones too, counts as -inf and hides no other class."""
+    rng = np.random.default_rng([n, classes, len(kind)])
+    unique = min(n, 10)
+    x = torch.from_numpy((rng.standard_normal((unique, classes)) * 3).astype(np.float32)).to(TYPES[kind])
+    as_bits, nans = NANS[kind]
+    bits = x.view(as_bits)
+    for r in range(unique):
+        share = (0.02, 0.2, 0.5, 0.97)[r % 4]
+        where = torch.from_numpy(rng.random(classes) < share)
+        some = nans if r % 3 == 0 else nans[r % 3 - 1::3]
+        bits[r, where] = torch.from_numpy(rng.choice(some, int(where.sum()))).to(as_bits)
+    bits[-1] = nans[0]
+    assert torch.isnan(x).any()
+    xd = x.repeat((n + unique - 1) // unique, 1)[:n].cuda()
+    for k in sorted({1, 3, min(48, classes), min(200, classes)}):
+        _check_top(sc, xd, _host(x), k, "NaN " + kind)
+    u = rng.random(unique).astype(np.float32)
+    ud = torch.from_numpy(u).cuda().repeat((n + unique - 1) // unique)[:n].contiguous()
+    for s in (dict(top_k=1), dict(top_k=40, top_p=0.9), dict(top_k=200), dict(temperature=0.0),
+              dict(top_p=0.8), dict(min_p=0.1)):
+        print("sample, NaN", kind, n, classes, s, flush=True)
+        got = _host(sc.sample(xd, ud, **s))
+        SU.check_sample(got[:unique], _host(x), u, **s, note=str(s))
+        np.testing.assert_array_equal(got, got[np.arange(n) % unique])
