@@ -303,14 +303,22 @@ class _Distill(torch.autograd.Function):
         x, values, index, stats = ctx.saved_tensors
         # on the stream of the forward pass; g may be a broadcast number (a sum's gradient)
         with _On(x, None, ()) as s:
-            if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+            n, classes = x.shape
+            ld, step = x.stride()
+            if step != 1 and classes > 1 or ld < classes and n > 1:
                 x = x.contiguous()
-            rows = _scores_arg(x, False)
+                ld = classes
             values, index, stats = values.contiguous(), index.contiguous(), stats.contiguous()
-            k = _teacher_arg(x, values, index)
-            _vector_arg(stats, "stats", (rows[2], 2), torch.float32, x.device)
-            grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            _gradient(rows, values, index, k, ctx.temperature, stats, g.contiguous(), grad, rows[3], s)
+            # (as _teacher_arg and _vector_arg check, whose 4 us a small call would feel)
+            device, shape = x.device, values.shape
+            if values.dtype != torch.float32 or index.dtype != torch.int32 or \
+                    stats.dtype != torch.float32 or len(shape) != 2 or shape[0] != n or \
+                    index.shape != shape or stats.shape != (n, 2) or x.dtype not in _TYPES or \
+                    values.device != device or index.device != device or stats.device != device:
+                raise ValueError("a saved tensor came back with another type, shape or device")
+            grad = torch.empty_like(x, memory_format=torch.contiguous_format)
+            _gradient((x.data_ptr(), _TYPES[x.dtype], n, classes, ld), values, index, shape[1],
+                      ctx.temperature, stats, g.contiguous(), grad, classes, s)
         return grad, None, None, None, None, None
 
 
