@@ -37,6 +37,7 @@ extern "C" {
 
 #define DS_MAX_CLASSES (1 << 20)   /* classes of a row */
 #define DS_MAX_TOP 256             /* k of ds_top_scores and of a teacher */
+#define DS_MAX_TEMPERATURE 1152921504606846976.0f   /* of ds_distill: 2^60 */
 
 /* Detailed message of the calling thread's last failed ds_* call ("" if none). */
 const char *ds_last_error(void);
@@ -106,17 +107,20 @@ dt_status ds_sample(const void *d_x, dt_dtype type, int64_t n, int32_t n_classes
  * score above -inf, has loss 0 and gradient 0.  A NaN or +inf among the student's scores makes
  * the row's loss and gradient NaN; one among the teacher's remaining values makes the loss, and
  * the gradient at the teacher's classes, NaN.  A teacher's class of some weight whose student's
- * score is -inf makes the loss +inf.
+ * score is -inf makes the loss +inf.  The loss, a difference
+ * of logarithms, is off by about 2^-22 t^2 however small it is, and more where scores are far
+ * apart.
  *   type       of the student's scores and of the gradient: DT_F32, DT_F16 or DT_BF16
  *   d_values, d_index   the teacher's entries, n rows of k, 1 <= k <= DS_MAX_TOP
+ *   temperature  positive: 4.5e-39 (1.5 / t is a number) .. DS_MAX_TEMPERATURE (t^2 is one)
  *   d_g        n floats; NULL: no gradient is computed (d_grad is then NULL as well)
  *   d_loss     n floats
  *   d_stats    n pairs of floats, aligned to 8, which ds_distill_backward takes: the row's
  *              largest score m and the sum of e^((x - m) / t)
  *   d_grad     n rows of n_classes, row stride ld_grad elements; must not overlap the scores
  *   d_work     workspace of at least ds_distill_work_bytes() bytes, aligned to 8 (NULL if 0)
- * Errors: as ds_top_scores; DT_ERR_INVALID_ARG also for a temperature that is not a positive
- * finite number, a workspace that is too small, or ld_grad < n_classes with n > 1.
+ * Errors: as ds_top_scores; DT_ERR_INVALID_ARG also for a temperature out of range, a workspace
+ * that is too small, or ld_grad < n_classes with n > 1.
  */
 dt_status ds_distill(const void *d_x, dt_dtype type, int64_t n, int32_t n_classes, int64_t ld,
                      const float *d_values, const int32_t *d_index, int32_t k, float temperature,

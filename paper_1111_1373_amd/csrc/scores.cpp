@@ -52,8 +52,8 @@ dt_status rows_of(const void *x, dt_dtype type, int64_t n, int32_t classes, int6
 dt_status teacher_of(const float *values, const int32_t *index, int32_t k, float temperature,
                      dscores::DistillArgs *a) {
     if (k < 1 || k > DS_MAX_TOP) return fail(DT_ERR_INVALID_ARG, "k must be 1 .. 256");
-    if (!(temperature > 0.0f && temperature <= 3.402823466e38f))
-        return fail(DT_ERR_INVALID_ARG, "temperature must be positive and finite");
+    if (!(temperature > 0.0f && temperature <= DS_MAX_TEMPERATURE))
+        return fail(DT_ERR_INVALID_ARG, "temperature must be positive and at most 2^60");
     if (!(1.5f / temperature <= 3.402823466e38f))      // log2 e over it is used
         return fail(DT_ERR_INVALID_ARG, "temperature is too small");
     if (a->in.n > 0 && (!values || !index)) return fail(DT_ERR_INVALID_ARG, "null teacher");

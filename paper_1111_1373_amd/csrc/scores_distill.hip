@@ -5,7 +5,9 @@
 // pass over a row finds m and s together: each thread keeps the largest score it has met and the
 // sum relative to it, scaled down when a larger one comes.  The gradient takes a second pass:
 // every class gets g t q_c, then the teacher's classes (at most 256 a row) are written again
-// with their share of p taken off.  An entry whose class another entry has too adds up all of
+// with their share of p taken off.  The loss is t times sum_j p_j ((v_j - top) - (x_j - m) + t (ln s - ln s_v)),
+// with the teacher's largest value and sum: nothing is divided by t, and t^2, which may be no fp32
+// number, is not needed.  An entry whose class another entry has too adds up all of
 // them in the entries' order, so both write the same number.
 #include "scores.hpp"
 #include "scores_common.hpp"
@@ -108,7 +110,6 @@ __device__ __forceinline__ bool teach(const DistillArgs &a, const Gr &g, int thr
                                       const Row<XT> &row, const Stats &st, const Entries &e,
                                       float *loss) {
     const float c2 = kLog2E / a.temperature;
-    const float inv = 1.0f / a.temperature;
     const float *values = a.values + r * a.k;
     const int32_t *index = a.index + r * a.k;
     float top = -__builtin_inff();
@@ -126,7 +127,8 @@ __device__ __forceinline__ bool teach(const DistillArgs &a, const Gr &g, int thr
         if (e.cls[j] >= 0) sum += power(e.p[j], top, c2);
     sum = g.reduce(sum, Sum());
     const bool any = !(sum == 0.0f);   // the best entry adds 1, a NaN a NaN
-    const float per_sum = 1.0f / sum, log_sums = MODE == kGradOnly ? 0.0f : logf(st.s) - logf(sum);
+    const float per_sum = 1.0f / sum;
+    const float log_sums = MODE == kGradOnly ? 0.0f : a.temperature * (logf(st.s) - logf(sum));
     float l = 0.0f;
     for (int j = g.thread; j < a.k; j += threads) {
         float p = 0.0f;
@@ -134,16 +136,16 @@ __device__ __forceinline__ bool teach(const DistillArgs &a, const Gr &g, int thr
         if (c >= 0) {
             p = power(e.p[j], top, c2) * per_sum;
             if constexpr (MODE != kGradOnly) {
-                // ln p - ln q
+                // t (ln p - ln q)
                 const float x = Elem<XT>::wide(row.p[c]) - finite(st.m);
-                if (p != 0.0f) l += p * (((e.p[j] - top) - x) * inv + log_sums);
+                if (p != 0.0f) l += p * (((e.p[j] - top) - x) + log_sums);
             }
         }
         e.p[j] = p;
     }
     if constexpr (MODE != kGradOnly) {
         l = g.reduce(l, Sum());
-        *loss = any && !st.empty() ? a.temperature * a.temperature * l : 0.0f;
+        *loss = any && !st.empty() ? a.temperature * l : 0.0f;
     }
     g.sync();                          // the entries are written
     return any;

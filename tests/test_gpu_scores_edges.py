@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests import scoreutil as SU
-from tests.test_gpu_scores import EPS, INF, TYPES, _host
+from tests.test_gpu_scores import EPS, INF, TYPES, _host, _teacher
 
 pytestmark = pytest.mark.gpu
 
@@ -191,3 +191,54 @@ def test_every_kind_of_nan(sc, n, classes, kind):
         got = _host(sc.sample(xd, ud, **s))
         SU.check_sample(got[:unique], _host(x), u, **s, note=str(s))
         np.testing.assert_array_equal(got, got[np.arange(n) % unique])
+
+
+@pytest.mark.parametrize("n,classes", [(40, 30), (20, 300), (8, 3_000), (3, 50_000)])
+@pytest.mark.parametrize("t", [1e-38, 1e-30, 1e-21, 1e-10, 1e-3, 1e3, 1e10, 2.0 ** 60])
+def test_distill_at_far_temperatures(sc, n, classes, t):
+    """Loss and gradient where t * t is no number of the type.  Tolerances as in _check_distill; below
+    2^-126 numbers are 2^-149 apart, and four operations of the loss round to them."""
+    rng = np.random.default_rng([n, classes])
+    x = (rng.standard_normal((n, classes)) * 3).astype(np.float32)
+    values, index = _teacher(rng, n, classes, 5)
+    g = (rng.random(n) + 0.5).astype(np.float32)
+    t = float(np.float32(t))
+    dev = [torch.from_numpy(v).cuda() for v in (x, values, index, g)]
+    print("distill", n, classes, t, flush=True)
+    for loss, grad in (sc.distill_grad(*dev, t),
+                       (lambda f: (f[0], sc.distill_backward(*dev[:3], f[1], dev[3], t)))(
+                           sc.distill_forward(*dev[:3], t))):
+        loss, grad = _host(loss).astype(np.float64), _host(grad).astype(np.float64)
+        want_l, want_g = SU.distill(x, values, index, t, g)
+        spread = np.ptp(x, axis=1) + np.ptp(np.where(np.isfinite(values), values, 0), axis=1)
+        spread = spread.astype(np.float64)
+        d = (spread / t + classes / 64 + 16) * 4 * EPS
+        tol = t * t * d * 2 + 2 * EPS * np.abs(want_l) + 4 * 2.0 ** -149
+        assert np.isfinite(loss).all()
+        assert (np.abs(loss - want_l) <= tol).all(), (loss, want_l)
+        # each of q and p is off by d of itself: their exponents by |z| eps, with z / t below 104 where
+        # they are not 0
+        d = (104 + classes / 64 + 16) * 4 * EPS
+        z = (x.astype(np.float64) - x.max(1, keepdims=True)) / t
+        q = np.exp(z) / np.exp(z).sum(1, keepdims=True)
+        p = np.abs(q * (t * g)[:, None] - want_g)
+        tol = ((t * g)[:, None] * q + p) * d * 2 + 2 * EPS * np.abs(want_g) + 2.0 ** -125
+        assert (np.abs(grad - want_g) <= tol).all(), np.abs(grad - want_g).max()
+
+
+@pytest.mark.parametrize("n,classes", [(9, 30), (5, 3_000)])
+def test_distill_of_far_scores(sc, n, classes):
+    """A class masked by the type's lowest value that the teacher has: the loss is a large number, as far
+    as there is one."""
+    rng = np.random.default_rng(classes)
+    lowest = float(np.finfo(np.float32).min)
+    x = rng.standard_normal((n, classes)).astype(np.float32)
+    x[:, 3] = lowest
+    values = np.zeros((n, 2), dtype=np.float32)
+    index = np.tile(np.array([[3, 1]], dtype=np.int32), (n, 1))
+    dev = [torch.from_numpy(v).cuda() for v in (x, values, index, np.ones(n, dtype=np.float32))]
+    for t in (0.25, 0.5, 1.0, 1.5):
+        print("distill, far scores", n, classes, t, flush=True)
+        loss = _host(sc.distill_grad(*dev, t)[0])
+        # t/2 times the lowest value, and what all else adds does not reach a step of it
+        np.testing.assert_allclose(loss, t / 2 * -lowest, rtol=16 * EPS)
