@@ -66,7 +66,8 @@ dt_status ds_top_scores(const void *d_x, dt_dtype type, int64_t n, int32_t n_cla
  *                their weight; at least the best; >= 1: all
  *   min_p        of these, only classes with w_c >= min_p stay (the best has 1); 0: all
  * Numbers outside these ranges are refused.  In arrays, which the call cannot see, they mean:
- * a temperature below 0 or NaN is 0, a top_p that is NaN is 1 and one below 0 is 0, a min_p
+ * a temperature below 0 or NaN is 0, one of +inf makes all classes equal in weight whose score is
+ * finite (if the best one's is), a top_p that is NaN is 1 and one below 0 is 0, a min_p
  * that is NaN or below 0 is 0 and one above 1 is 1.
  */
 typedef struct {

@@ -248,21 +248,32 @@ struct WideSpace {
 };
 
 // A class's place on a scale of kNats / kBins steps below the best: the larger the score the
-// lower the bin (each step of the computation keeps the order); kBins for weight 0.
+// lower the bin (each step of the computation keeps the order); kBins for weight 0.  The difference from
+// the best is taken of scores times a power of two: 1, but 1/2 where it may pass the largest fp32 number,
+// and 2^64 where the temperature's reciprocal may, which then counts for small scores alone (others are either
+// equal or at least 2^36 apart).
 template <dt_dtype XT, int WAVES>
 struct Scale {
     using W = Weights<XT>;
     const W &w;
-    float step;
-    __device__ __forceinline__ explicit Scale(const W &weights)
-        : w(weights), step(float(weights.inv * (bins_of(WAVES) / kNats))) {}
+    float unit, base, step;
+    __device__ __forceinline__ explicit Scale(const W &weights) : w(weights), unit(1.0f) {
+        if constexpr (!W::kVotes) {
+            if (w.best >= 0x1p102f)
+                unit = 0.5f;
+            else if (w.inv > 0x1p100 && fabsf(w.best) < 0x1p60f)
+                unit = 0x1p64f;
+            base = w.best * unit;
+        }
+        step = float(w.inv * (bins_of(WAVES) / kNats) / unit);
+    }
     __device__ __forceinline__ int bin(typename W::Read x) const {
         constexpr int n = bins_of(WAVES);
         float diff;
         if constexpr (W::kVotes)
             diff = float(w.m) - float(w.ln[x]);
         else
-            diff = w.best - x;
+            diff = fmaf(x, -unit, base);
         const float d = x == w.best ? 0.0f : diff * step;
         return d < float(n) ? int(d) : n;                            // n for a NaN
     }

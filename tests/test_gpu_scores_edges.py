@@ -242,3 +242,60 @@ def test_distill_of_far_scores(sc, n, classes):
         loss = _host(sc.distill_grad(*dev, t)[0])
         # t/2 times the lowest value, and what all else adds does not reach a step of it
         np.testing.assert_allclose(loss, t / 2 * -lowest, rtol=16 * EPS)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [60, 900, 3_000, 30_000])
+def test_sample_at_the_ends_of_the_types(sc, kind, classes):
+    """Scores whose differences are no fp32 numbers, at temperatures at which these classes are drawn,
+    and scores below 2^-126 at temperatures like them."""
+    rng = np.random.default_rng([classes, len(kind)])
+    n = 12
+    most = torch.finfo(TYPES[kind]).max
+    wide = torch.from_numpy(rng.uniform(-1, 1, (n, classes))) * most
+    wide[1] = torch.from_numpy(rng.choice([-1.0, 1.0], classes)) * most
+    wide[2] = -most
+    wide[2, 5] = most
+    wide[3, ::2] = -INF
+    least = torch.from_numpy(rng.uniform(-1, 1, (n, classes))) * 2.0 ** -120
+    least[1] *= 2.0 ** -12                                  # below 2^-126
+    least[2, :] = -most
+    least[2, 7:11] = -2.0 ** -120
+    least[3, ::2] = -INF
+    for x, ts in ((wide, (3e37, 1e38, 3.4e38)), (least, (1e-37, 2e-37, 1e-38, 2e-40, 1e-45))):
+        x = x.to(TYPES[kind])
+        u = rng.random(n).astype(np.float32)
+        xd, ud = x.cuda(), torch.from_numpy(u).cuda()
+        for t in ts:
+            for s in (dict(top_p=0.5), dict(top_k=classes // 2), dict(top_k=classes // 2, top_p=0.8),
+                      dict(), dict(min_p=0.3, top_p=0.99)):
+                print("sample, ends", kind, classes, t, s, flush=True)
+                SU.check_sample(_host(sc.sample(xd, ud, t, **s)), _host(x), u, t, **s,
+                                note="%s %s" % (t, s))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "u8"])
+@pytest.mark.parametrize("classes", [60, 900, 3_000])
+def test_sample_at_infinite_temperature(sc, kind, classes):
+    """Only an array can hold it: all classes with a score weigh the same."""
+    rng = np.random.default_rng([classes, len(kind)])
+    n = 10
+    if kind == "u8":
+        x = torch.from_numpy(rng.integers(1, 40, (n, classes)).astype(np.uint8))
+    else:
+        x = (torch.from_numpy(rng.uniform(-1, 1, (n, classes))) * torch.finfo(TYPES[kind]).max).to(TYPES[kind])
+    t = torch.full((n,), INF, device="cuda")
+    u = rng.random(n).astype(np.float32)
+    ud = torch.from_numpy(u).cuda()
+    for s in (dict(top_p=0.5), dict(top_k=classes // 2), dict(top_k=30, top_p=0.5), dict(min_p=1.0)):
+        print("sample, infinite temperature", kind, classes, s, flush=True)
+        SU.check_sample(_host(sc.sample(x.cuda(), ud, t, **s)), _host(x), u, INF, **s)
+    if kind != "u8":
+        x[:, ::3] = -INF
+        x[:, 1::3] = float("nan")
+    else:
+        x[:, ::3] = 0
+        x[:, 1::3] = 0
+    for s in (dict(top_p=0.7), dict()):
+        got = _host(sc.sample(x.cuda(), ud, t, **s))
+        assert (got % 3 == 2).all()
