@@ -52,8 +52,8 @@ __global__ void __launch_bounds__(256) top_lanes(TopArgs a) {
         }
 }
 
-// ln 2^y for the sum: e^(x - m) = 2^(x log2 e - m log2 e), whose second product is the same for the
-// whole row.  Its rounding moves the sum's logarithm by at most half a step of m.
+// e^(x - m) = 2^(x log2 e - m log2 e), whose second product is the same for the whole row.  So is its
+// rounding error, up to 0.7 steps of m in the sum's logarithm, which log() puts back.
 struct Exponent {
     float base, shift;     // m, -m log2 e
     __device__ __forceinline__ void set(float m) {
@@ -62,6 +62,10 @@ struct Exponent {
     }
     __device__ __forceinline__ float operator()(float x) const {
         return __builtin_amdgcn_exp2f(fmaf(x, 1.44269504f, shift));
+    }
+    // of a sum of terms, with e^m
+    __device__ __forceinline__ float log(float sum) const {
+        return base + fmaf(fmaf(-base, 1.44269504f, -shift), 0.693147181f, logf(sum));
     }
 };
 
@@ -120,7 +124,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES >= 4 ? 4 
                 if (best == __builtin_inff()) {
                     lse = best;
                 } else if (sum < 1e30f && fabsf(ex.base) <= 1e6f) {
-                    lse = ex.base + logf(sum);
+                    lse = ex.log(sum);
                 } else {
                     // The best is far above the stretch that the sum is relative to, or so large
                     // that the rounding of m log2 e is, or there is a NaN: again, term by term.

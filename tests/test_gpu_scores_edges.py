@@ -299,3 +299,22 @@ def test_sample_at_infinite_temperature(sc, kind, classes):
     for s in (dict(top_p=0.7), dict()):
         got = _host(sc.sample(x.cuda(), ud, t, **s))
         assert (got % 3 == 2).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [100, 1000, 5_000, 40_000])
+def test_log_sum_of_a_sure_row(sc, kind, classes):
+    """One class far above the others: the log-sum-exp is its score.  The sum is 1 but for the
+    exponential's error (one step of 2^-23) and the classes that are 60 below it, so its logarithm is off by
+    at most 2^-22, and scores from 16 on are 2^-19 apart at least."""
+    rng = np.random.default_rng(classes)
+    n = 400 if classes <= 5_000 else 60
+    m = rng.uniform(16, 1000, n) * rng.choice([-1.0, 1.0], n)
+    m[: n // 4] *= 1000
+    m = torch.from_numpy(m).to(TYPES[kind])
+    x = (m.double()[:, None] - 60 - torch.from_numpy(rng.random((n, classes))) * 20 - m.double().abs()[:, None] / 64)
+    x = x.to(TYPES[kind])
+    x[torch.arange(n), torch.from_numpy(rng.integers(0, classes, n))] = m
+    print("sure rows", kind, classes, flush=True)
+    lse = _host(sc.top_scores(x.cuda(), 1)[2])
+    np.testing.assert_array_equal(lse, _host(m).astype(np.float32))
