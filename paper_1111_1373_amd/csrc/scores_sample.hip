@@ -80,8 +80,10 @@ struct Weights {
         else
             return Elem<XT>::wide(e);
     }
-    __device__ __forceinline__ Weights(const Settings &s, uint32_t top_key, const double *ln_table)
+    template <int N>
+    __device__ __forceinline__ Weights(const Settings &s, uint32_t top_key, const double (&ln_table)[N])
         : top(top_key), inv(s.inv), counts(s.counts), ln(ln_table) {
+        static_assert(!kVotes || N == 256, "votes look up their logarithms");
         if constexpr (kVotes) {
             best = top;
             m = ln[top];
@@ -161,15 +163,23 @@ __global__ void __launch_bounds__(256) sample_lanes(SampleArgs a) {
         a.labels[row] = -1;
         return;
     }
-    const Weights<XT> weights(set, O::key(first), ln);
+    const auto weights = [&] {
+        if constexpr (COUNTS)
+            return 0;                      // not needed
+        else
+            return Weights<XT>(set, O::key(first), ln);
+    }();
     auto weight = [&](uint32_t key) -> Sum {
         if constexpr (COUNTS)
             return key;
         else
             return weights(key);
     };
-    const Sum least = COUNTS ? Sum(__builtin_ceil(set.min_p * double(O::key(first))))
-                             : Sum(weights.least(set.min_p));
+    Sum least;
+    if constexpr (COUNTS)
+        least = Sum(__builtin_ceil(set.min_p * double(O::key(first))));
+    else
+        least = weights.least(set.min_p);
     typename O::T cut = 0;                 // classes from here on stay, in their order
     Sum sum = 0;
     if (set.k < n || set.p < 1.0) {
