@@ -241,8 +241,12 @@ def _grad_out(x, out):
     if out is not None and out.numel() and x.untyped_storage().data_ptr() == \
             out.untyped_storage().data_ptr():
         lo, hi = sorted((x, out), key=lambda t: t.data_ptr())
-        if lo.data_ptr() + lo.element_size() * ((lo.shape[0] - 1) * lo.stride(0) + lo.shape[1]) \
-                > hi.data_ptr():
+        size, ld = lo.element_size(), lo.stride(0)
+        off = hi.data_ptr() - lo.data_ptr()
+        # columns of one matrix lie beside each other
+        beside = ld == hi.stride(0) and ld > 0 and \
+            lo.shape[1] <= off % (ld * size) // size <= ld - lo.shape[1]
+        if off < size * ((lo.shape[0] - 1) * ld + lo.shape[1]) and not (lo.shape[0] > 1 and beside):
             raise ValueError("out must not overlap the scores, which are read again")
 
 

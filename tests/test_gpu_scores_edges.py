@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests import scoreutil as SU
-from tests.test_gpu_scores import EPS, INF, TYPES, _host, _teacher
+from tests.test_gpu_scores import EPS, INF, TYPES, _check_distill, _host, _teacher
 
 pytestmark = pytest.mark.gpu
 
@@ -318,3 +318,41 @@ def test_log_sum_of_a_sure_row(sc, kind, classes):
     print("sure rows", kind, classes, flush=True)
     lse = _host(sc.top_scores(x.cuda(), 1)[2])
     np.testing.assert_array_equal(lse, _host(m).astype(np.float32))
+
+
+@pytest.mark.parametrize("n,classes", [(5, 20), (7, 300), (4, 9_000), (1, 9_000)])
+def test_gradient_beside_the_scores(sc, n, classes):
+    """Scores and gradient as columns of one matrix: they do not overlap.  Those that do are refused."""
+    rng = np.random.default_rng(classes)
+    both = torch.full((n, 2 * classes + 6), 3.0, device="cuda")
+    x, out = both[:, :classes], both[:, classes + 3:2 * classes + 3]
+    x.copy_(torch.from_numpy(rng.standard_normal((n, classes)).astype(np.float32)))
+    teacher = _teacher(rng, n, classes, 4)
+    values, index = (torch.from_numpy(v).cuda() for v in teacher)
+    g = torch.ones(n, device="cuda")
+    for a, b in ((x, out), (out, x)):
+        keep = x.clone()
+        b.fill_(0)
+        a.copy_(keep)
+        print("beside", n, classes, flush=True)
+        loss, grad = sc.distill_grad(a, values, index, g, 2.0, out=b)
+        assert grad is b
+        _check_distill(_host(keep), *teacher, 2.0, _host(g), _host(loss), _host(b), "f32")
+        np.testing.assert_array_equal(_host(a), _host(keep))
+        b.fill_(0)
+        loss, stats = sc.distill_forward(a, values, index, 2.0)
+        sc.distill_backward(a, values, index, stats, g, 2.0, out=b)
+        _check_distill(_host(keep), *teacher, 2.0, _host(g), _host(loss), _host(b), "f32")
+        x.copy_(keep)
+    assert (both[:, classes: classes + 3] == 3).all() and (both[:, 2 * classes + 3:] == 3).all()
+    for off in (0, 1, classes - 1):
+        with pytest.raises(ValueError):
+            sc.distill_grad(x, values, index, g, 2.0, out=both[:, off:off + classes])
+    flat = torch.zeros((n + 1) * (classes + 2), device="cuda")
+    a = flat[:n * (classes + 2)].view(n, classes + 2)[:, :classes]
+    # from the middle of a row on, and from a row's end into the next one's scores
+    for off in (classes // 2 + 2, classes, classes + 1):
+        b = flat[off:][:n * (classes + 2)].view(n, classes + 2)[:, :classes]
+        if n > 1 or off < classes:
+            with pytest.raises(ValueError):
+                sc.distill_grad(a, values, index, g, 2.0, out=b)
