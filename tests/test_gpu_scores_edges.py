@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 
 from tests import scoreutil as SU
-from tests.test_gpu_scores import EPS, INF, TYPES, _check_distill, _host, _teacher
+from tests.test_gpu_scores import (EPS, HALF_STEP, INF, TYPES, _check_distill, _host, _scores,
+                                    _strided, _teacher)
 
 pytestmark = pytest.mark.gpu
 
@@ -356,3 +357,61 @@ def test_gradient_beside_the_scores(sc, n, classes):
         if n > 1 or off < classes:
             with pytest.raises(ValueError):
                 sc.distill_grad(a, values, index, g, 2.0, out=b)
+
+
+@pytest.mark.parametrize("how", ["dense", "strided"])
+@pytest.mark.parametrize("kind,classes", [("f32", 16_380), ("f32", 16_381), ("f32", 32_765),
+                                          ("f32", 65_532), ("f32", 65_533), ("f16", 32_761),
+                                          ("f16", 65_529), ("f16", 131_064), ("f16", 131_065),
+                                          ("bf16", 40_001), ("bf16", 70_003), ("bf16", 140_000)])
+def test_distill_many_long_rows(sc, kind, classes, how):
+    """Loss and gradient in one call, around the lengths at which the number of threads changes and at which
+    a row no longer fits their registers."""
+    rng = np.random.default_rng([classes, len(kind)])
+    unique, n, k = 12, 516, 100
+    x = (rng.standard_normal((unique, classes)) * 3).astype(np.float32)
+    x[2::5, ::3] = -INF
+    x[4] = -INF
+    x[5, 7] = np.nan
+    x[6, classes // 2] = INF
+    x = torch.from_numpy(x).to(TYPES[kind])
+    teacher = _teacher(rng, unique, classes, k)
+    g = (rng.standard_normal(unique) * 2).astype(np.float32)
+    values, index, gd = (torch.from_numpy(np.tile(v, (n // unique,) + (1,) * (v.ndim - 1))).cuda()
+                         for v in (*teacher, g))
+    xd = _strided(x.repeat(n // unique, 1).cuda(), how)
+    print("distill, many long rows", kind, classes, how, flush=True)
+    loss, grad = sc.distill_grad(xd, values, index, gd, 1.5)
+    rows = np.sort(rng.choice(n, 24, replace=False))
+    rows[[0, -1]] = 0, n - 1
+    at = rows % unique
+    _check_distill(_host(x)[at], *(v[at] for v in teacher), 1.5, g[at], _host(loss)[rows],
+                   _host(grad[torch.from_numpy(rows).cuda()]), kind)
+    # Nothing of any row is left out: its gradient sums up to the same as its first copy's.  Each element is
+    # off by half a step of its type, d of itself (as in _check_distill, with a spread below 64), and half of
+    # the type's smallest number, on both sides.
+    sums, size = grad.double().sum(1), grad.double().abs().sum(1)
+    d = (64 + classes / 64 + 16) * 4 * EPS + HALF_STEP[kind]
+    tol = 2 * (d * size + classes * (2.0 ** -25 if kind == "f16" else 2.0 ** -126))
+    first = sums[:unique].repeat(n // unique)
+    assert bool(((sums - first).abs() <= tol)[~first.isnan()].all())
+    assert torch.equal(sums.isnan(), first.isnan())
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "u8"])
+@pytest.mark.parametrize("n,classes", [(300, 20_000), (1100, 20_000), (1100, 131_080)])
+def test_many_long_rows(sc, n, classes, kind):
+    """Teams of 4 and 8 wavefronts on long rows."""
+    rng = np.random.default_rng([n, classes, len(kind)])
+    rows = _scores(rng, 9, classes, kind)
+    x = rows.repeat(n // 9 + 1, 1)[:n].contiguous()
+    for k in (1, 64, 96, 97, 256):
+        _check_top(sc, x, _host(rows), k, "many long rows " + kind)
+    u = rng.random(9).astype(np.float32)
+    ud = torch.from_numpy(u).cuda().repeat(n // 9 + 1)[:n].contiguous()
+    for s in (dict(top_k=1), dict(top_k=96, top_p=0.9), dict(top_k=97), dict(top_k=256, temperature=2.0),
+              dict(top_p=0.8), dict(top_k=300, top_p=0.9), dict()):
+        print("sample, many long rows", kind, n, classes, s, flush=True)
+        got = _host(sc.sample(x, ud, **s))
+        SU.check_sample(got[:9], _host(rows), u, **s, note=str(s))
+        np.testing.assert_array_equal(got, got[np.arange(n) % 9])
