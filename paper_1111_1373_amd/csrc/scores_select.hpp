@@ -150,7 +150,8 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, 
         top = v[i] > top ? v[i] : top;
         if (64 * i < parts) lo = v[i] < lo ? v[i] : lo;
     }
-    uint32_t hi = wave_reduce(top, Max()) + 1;                   // none reaches hi
+    top = wave_reduce(top, Max());
+    uint32_t hi = top + (top != ~0u);                            // none reaches hi (but fp32's +inf)
     lo = wave_reduce(lo, Min());                                 // and all reach lo
     lo = lo > least ? lo : least;
     auto reach = [&](uint32_t x) {
@@ -160,7 +161,7 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int parts, 
             if (64 * i < parts) n += __popcll(__ballot(v[i] >= x));
         return n;
     };
-    if (hi <= lo || reach(lo) < k) return least;
+    if (lo > top || reach(lo) < k) return least;
     while (hi - lo > 1) {
         const uint32_t mid = lo + ((hi - lo) >> 1);
         const int n = reach(mid);
