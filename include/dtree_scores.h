@@ -23,7 +23,7 @@
  * nothing else (no allocation, copy, memset or synchronisation), so it may be captured in a
  * HIP graph.  Buffers are the caller's and must stay valid until the work completes; calls
  * that may run at the same time need workspaces of their own, calls that follow each other on
- * a stream may share one.  n == 0 launches nothing.  Nothing is written on an error return.
+ * a stream may share one.  Outputs overlap neither each other nor an input.  n == 0 launches nothing.  Nothing is written on an error return.
  * All calls are noexcept; ds_last_error() has the last error's message of the calling thread.
  */
 #ifndef DTREE_SCORES_H

@@ -23,6 +23,10 @@ constexpr int kQuarter = 96;
 // The same for one wavefront, on rows of at most 1,024 classes (60,000 rows of 1,000 bf16, k = 48:
 // 305 us, 429 with 4 wavefronts; k = 60: 502 and 476; fp32, k = 200: 1,725 and 953).
 constexpr int kSixteenth = 48;
+// The sampler's teams are chosen by the same numbers, but without one of 8 where most classes stay:
+// 64 rows of 5,000 bf16 by top-p in 25 us with 4 wavefronts and 27 with 16, of 9,000 in 33 and 31;
+// 256 of 131,072 in 298 and 149, 512 of 32,768 in 91 and 103, 1,024 in 126 and 191.  Just above 256
+// rows 16 would still be faster on the longest (300 of 131,072: 328 and 242).
 
 struct RowArgs {
     const void *x;

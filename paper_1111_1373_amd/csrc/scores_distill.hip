@@ -362,8 +362,14 @@ void run_rows(const DistillArgs &a, hipStream_t stream) {
                                 Group<G>::kThreads, 0, stream>>>(a);
 }
 
-// Rows for 8 lanes: few classes, and no more of the teacher's entries than they have room for.
+// Rows for 8 lanes: few classes, and no more of the teacher's entries than they have room for
+// (1,000,000 x 32 fp32, k = 4, one call: 83 us, 539 with a wavefront a row).
 bool small(const DistillArgs &a) { return a.in.classes <= kLaneClasses && a.k <= kLaneClasses; }
+
+// Rows for a wavefront: 30,000 x 2,048 bf16, k = 32, one call: 68 us, 236 with 256 threads a row; on longer
+// ones the gain ends with the type (15,000 x 4,096 bf16 73 and 128, fp32 133 and 149, fp32's backward pass alone
+// 106 and 97).
+constexpr int kWaveClasses = 2048;
 
 template <dt_dtype XT>
 void run_backward(DistillArgs a, hipStream_t stream) {
@@ -371,7 +377,7 @@ void run_backward(DistillArgs a, hipStream_t stream) {
     a.parts = 1;
     if (small(a)) {
         run_rows<XT, 8, kGradOnly>(a, stream);
-    } else if (c <= 2048) {
+    } else if (c <= kWaveClasses) {
         run_rows<XT, 64, kGradOnly>(a, stream);
     } else {
         a.parts = distill_parts(a.in.n, c);
@@ -390,7 +396,7 @@ void run(const DistillArgs &a, hipStream_t stream) {
     } else if (small(a)) {
         if (a.g) run_rows<XT, 8, kBoth>(a, stream);
         else run_rows<XT, 8, kLossOnly>(a, stream);
-    } else if (c <= 2048) {
+    } else if (c <= kWaveClasses) {
         if (a.g) run_rows<XT, 64, kBoth>(a, stream);
         else run_rows<XT, 64, kLossOnly>(a, stream);
     } else if (!a.g) {
@@ -407,7 +413,14 @@ void run(const DistillArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// Parts of a row: as many as fill the card with workgroups, of 4,096 classes at least.
+// Parts of a row: as many as fill the card with workgroups, of 4,096 classes at least.  They cost the loss
+// a second launch and save the backward pass its time on few compute units: 100 x 32,768 bf16, k = 64,
+// loss 15 us and backward 13, without parts 11 and 17; 256 x 131,072: 18 and 29, 18 and 40; 600 x
+// 131,072: 31 and 59 both ways.  Loss and gradient in one call gain on the longest rows (256 x 131,072:
+// 47 us, 56 without parts) and lose on others, which then stay in registers (500 x 50,000: 39 and 28).
+// Parts of 2,048 to 16,384 classes, and 512 to 2,048 workgroups, take the same within 1 us (1 to 128
+// rows of 131,072); of one row of 1,000,000 the backward pass takes 15.3 us with 32 parts at most, 12.6
+// with 64 and 12.4 with 128.
 int distill_parts(int64_t n, int32_t classes) {
     if (n >= 512 || classes <= 8192) return 1;
     const int64_t want = (1024 + n - 1) / n, most = classes / 4096;

@@ -4,7 +4,8 @@
 // borders of top-p; with many classes the sums' rounding would decide it.  Weights are
 // therefore computed in 64 bits and rounded once to whole multiples of 2^-42 of the largest
 // one, and added as 64-bit integers (at most 2^20 of them): every order of summation gives the
-// same sum, so the lanes, wavefronts and atomics that share a row cannot change a result.
+// same sum, so the lanes, wavefronts and atomics that share a row cannot change a result.  It is fewer bits
+// than a sum in fp64 has (53): a share or a random number within n 2^-41 of a border may fall on its other side.
 #include "scores.hpp"
 #include "scores_lanes.hpp"
 #include "scores_select.hpp"

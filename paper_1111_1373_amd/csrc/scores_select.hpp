@@ -5,9 +5,10 @@
 // classes do, and few more do (of 256 parts and k = 64, about 74).  A second walk collects what
 // reaches the bound, and only that is put in order.  The parts may cover a stretch of the row alone:
 // with k of its maxima above a bound, the whole row has about (row / stretch) times as many
-// classes above it.  The stretch stays in the LDS, as far as it fits, so the row is read from memory
-// once.  2,048 rows of 131,072 bf16, k = 64, with their log-sum-exp: 118 us = 4.6 TB/s (a read alone
-// reaches 6.9); of a row's 52 us with three others on its compute unit, 44 are the two walks, bound by
+// classes above it.  The stretch stays in the LDS as far as it fits and is read again beyond that: of
+// 131,072 bf16 with k = 64 a team of 4 wavefronts looks at 4,369 vectors first and keeps 1,280, so 1.2
+// times the row crosses the memory.  2,048 such rows with their log-sum-exp: 118 us = 4.6 TB/s of the rows' bytes
+// (a read alone reaches 6.9); of a row's 52 us with three others on its compute unit, 44 are the two walks, bound by
 // loads and by the exponentials' instructions, and 6 finding the bounds and collecting.
 #pragma once
 
