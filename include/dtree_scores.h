@@ -21,10 +21,11 @@
  * Calls are asynchronous on `stream` (a hipStream_t; NULL = the null stream) of the current
  * device, which the buffers must belong to.  A call puts kernel launches on the stream and
  * nothing else (no allocation, copy, memset or synchronisation), so it may be captured in a
- * HIP graph.  Buffers are the caller's and must stay valid until the work completes; calls
- * that may run at the same time need workspaces of their own, calls that follow each other on
- * a stream may share one.  Outputs overlap neither each other nor an input.  n == 0 launches nothing.  Nothing is written on an error return.
- * All calls are noexcept; ds_last_error() has the last error's message of the calling thread.
+ * HIP graph.  Buffers are the caller's and must stay valid until the work completes; outputs
+ * overlap neither each other nor an input; calls that may run at the same time need workspaces of
+ * their own, calls that follow each other on a stream may share one.  n == 0 launches nothing.
+ * Nothing is written on an error return.  All calls are noexcept; ds_last_error() has the last
+ * error's message of the calling thread.
  */
 #ifndef DTREE_SCORES_H
 #define DTREE_SCORES_H

@@ -415,3 +415,16 @@ def test_many_long_rows(sc, n, classes, kind):
         got = _host(sc.sample(x, ud, **s))
         SU.check_sample(got[:9], _host(rows), u, **s, note=str(s))
         np.testing.assert_array_equal(got, got[np.arange(n) % 9])
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("classes", [8, 31, 62, 64, 65, 700])
+def test_log_sum_of_equal_small_terms(sc, classes, kind):
+    """One class above many equal ones, whose terms are all rounded the same way in a running sum."""
+    rng = np.random.default_rng([classes, len(kind)])
+    n = 1000
+    x = np.repeat(-rng.uniform(1, 9, (n, 1)), classes, 1).astype(np.float32)
+    x[np.arange(n), rng.integers(0, classes, n)] = 0
+    x += rng.integers(-3, 4, (n, 1)).astype(np.float32)
+    rows = torch.from_numpy(x).to(TYPES[kind])
+    _check_top(sc, rows.cuda(), _host(rows), 1, "equal terms " + kind)
