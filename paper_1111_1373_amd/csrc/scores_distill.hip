@@ -5,10 +5,12 @@
 // pass over a row finds m and s together: each thread keeps the largest score it has met and the
 // sum relative to it, scaled down when a larger one comes.  The gradient takes a second pass:
 // every class gets g t q_c, then the teacher's classes (at most 256 a row) are written again
-// with their share of p taken off.  The loss is t times sum_j p_j ((v_j - top) - (x_j - m) + t (ln s - ln s_v)),
-// with the teacher's largest value and sum: nothing is divided by t, and t^2, which may be no fp32
-// number, is not needed.  An entry whose class another entry has too adds up all of
+// with their share of p taken off.  An entry whose class another entry has too adds up all of
 // them in the entries' order, so both write the same number.
+//
+// The loss is t times sum_j p_j ((v_j - top) - (x_j - m) + t (ln s - ln s_v)), with the teacher's
+// largest value and its sum: nothing is divided by t, and t^2, which may be no fp32 number, is not
+// needed.
 #include "scores.hpp"
 #include "scores_common.hpp"
 
@@ -366,9 +368,9 @@ void run_rows(const DistillArgs &a, hipStream_t stream) {
 // (1,000,000 x 32 fp32, k = 4, one call: 83 us, 539 with a wavefront a row).
 bool small(const DistillArgs &a) { return a.in.classes <= kLaneClasses && a.k <= kLaneClasses; }
 
-// Rows for a wavefront: 30,000 x 2,048 bf16, k = 32, one call: 68 us, 236 with 256 threads a row; on longer
-// ones the gain ends with the type (15,000 x 4,096 bf16 73 and 128, fp32 133 and 149, fp32's backward pass alone
-// 106 and 97).
+// Rows for a wavefront: 30,000 x 2,048 bf16, k = 32, one call: 68 us, 236 with 256 threads a row; on
+// longer ones the gain ends with the type (15,000 x 4,096 bf16 73 and 128, fp32 133 and 149, fp32's
+// backward pass alone 106 and 97).
 constexpr int kWaveClasses = 2048;
 
 template <dt_dtype XT>

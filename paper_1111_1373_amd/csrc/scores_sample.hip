@@ -4,8 +4,9 @@
 // borders of top-p; with many classes the sums' rounding would decide it.  Weights are
 // therefore computed in 64 bits and rounded once to whole multiples of 2^-42 of the largest
 // one, and added as 64-bit integers (at most 2^20 of them): every order of summation gives the
-// same sum, so the lanes, wavefronts and atomics that share a row cannot change a result.  It is fewer bits
-// than a sum in fp64 has (53): a share or a random number within n 2^-41 of a border may fall on its other side.
+// same sum, so the lanes, wavefronts and atomics that share a row cannot change a result.  It is
+// fewer bits than a sum in fp64 has (53): a share or a random number within n 2^-41 of a border may
+// fall on its other side.
 #include "scores.hpp"
 #include "scores_lanes.hpp"
 #include "scores_select.hpp"
@@ -260,9 +261,9 @@ struct WideSpace {
 
 // A class's place on a scale of kNats / kBins steps below the best: the larger the score the
 // lower the bin (each step of the computation keeps the order); kBins for weight 0.  The difference from
-// the best is taken of scores times a power of two: 1, but 1/2 where it may pass the largest fp32 number,
-// and 2^64 where the temperature's reciprocal may, which then counts for small scores alone (others are either
-// equal or at least 2^36 apart).
+// the best is taken of scores times a power of two: 1, but 1/2 where it may pass the largest fp32
+// number, and 2^64 where the temperature's reciprocal may, which then counts for small scores
+// alone (others are either equal or at least 2^36 apart).
 template <dt_dtype XT, int WAVES>
 struct Scale {
     using W = Weights<XT>;

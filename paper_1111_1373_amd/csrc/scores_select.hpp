@@ -6,10 +6,11 @@
 // reaches the bound, and only that is put in order.  The parts may cover a stretch of the row alone:
 // with k of its maxima above a bound, the whole row has about (row / stretch) times as many
 // classes above it.  The stretch stays in the LDS as far as it fits and is read again beyond that: of
-// 131,072 bf16 with k = 64 a team of 4 wavefronts looks at 4,369 vectors first and keeps 1,280, so 1.2
-// times the row crosses the memory.  2,048 such rows with their log-sum-exp: 118 us = 4.6 TB/s of the rows' bytes
-// (a read alone reaches 6.9); of a row's 52 us with three others on its compute unit, 44 are the two walks, bound by
-// loads and by the exponentials' instructions, and 6 finding the bounds and collecting.
+// 131,072 bf16 with k = 64 a team of 4 wavefronts looks at 4,369 vectors first and keeps 1,280,
+// so 1.2 times the row crosses the memory.  2,048 such rows with their log-sum-exp: 118 us =
+// 4.6 TB/s of the rows' bytes (a read alone reaches 6.9); of a row's 52 us with three others on its
+// compute unit, 44 are the two walks, bound by loads and by the exponentials' instructions, and 6
+// finding the bounds and collecting.
 #pragma once
 
 #include "scores_common.hpp"
@@ -52,8 +53,8 @@ struct Collected {
 };
 
 // list[0 .. c) in descending order, in place: a bitonic network over the next power of two (at
-// least 64), for which the list has room, and whose places behind c hold 0 (smaller than any class that is
-// collected).
+// least 64), for which the list has room, and whose places behind c hold 0 (smaller than any
+// class that is collected).
 template <int WAVES>
 __device__ __forceinline__ void sort_list(const Team<WAVES> &t, uint64_t *list, int c) {
     int n = 64;
